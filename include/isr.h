@@ -177,6 +177,104 @@ int isr_noise_bank_static(uint32_t sigma, uint64_t seed, uint32_t bank_id, uint3
                           uint32_t d, int16_t *out_device, void *hip_stream);
 size_t isr_noise_bank_static_capacity(void);
 
+/* ---- operators on rows of class logits ------------------------------------- */
+
+/* What a classifier answers with, a row of logits per copy (or token, over the classes of its
+ * vocabulary), turned into log-probabilities, and the loss that trains one classifier on the
+ * top logits of another, e.g. the int8 network's on the fp32 network's.  Both work on logits in
+ * device memory, are enqueued on hip_stream (NULL = default; of the current device, which is the
+ * one that holds the memory) and return at once: no allocation, no copy, no synchronisation, so
+ * a call can be captured into a graph.  Workspaces hold nothing between calls; calls that may
+ * overlap in time need a workspace each.  Results do not depend on the order in which workgroups
+ * run.  Sums and statistics are fp32 or wider.
+ *
+ * Logits x[r][j], j < classes, element (r, j) at data_device + r * row_stride + j (in elements);
+ * aligned to their element, no more.  l = scale * x: scale is 1 / temperature, times the step of
+ * one unit for int32 logits of an int8 network.  A float logit of -infinity marks an impossible
+ * class.  A row without a possible class is empty.  A row that holds NaN or +infinity has NaN as
+ * its results and -1 for each class asked for. */
+#define ISR_F32 0
+#define ISR_BF16 1
+#define ISR_F16 2
+#define ISR_I32 3
+
+typedef struct isr_logits {
+    const void *data_device;
+    int32_t type;        /* ISR_F32, ISR_BF16, ISR_F16 or ISR_I32 */
+    uint32_t classes;    /* 1 .. 2^24 */
+    uint64_t rows;       /* 0 .. 2^31 - 1 */
+    uint64_t row_stride; /* elements, >= classes */
+    float scale;         /* finite, > 0 */
+} isr_logits;
+
+#define ISR_MAX_GIVEN 128 /* given classes a row, and entries of the teacher */
+#define ISR_MAX_TOP 128   /* top alternatives a row, at most classes */
+
+/* log p_j = l_j - log sum_i exp l_i of the `given` classes of each row, the row's entropy
+ * -sum_j p_j log p_j (nats), and its `top` most likely classes with their log-probabilities, in
+ * descending order, equal logits by ascending class.
+ *   given_device          int32 [rows][given]; a negative one does not count (log-probability 0),
+ *                         one >= classes gives NaN; may name a class twice
+ *   logprob_device        float [rows][given]
+ *   entropy_device        float [rows] or NULL
+ *   top_class_device      int32 [rows][top], top_logprob_device float [rows][top]: -1 and
+ *                         -infinity from where the row has no further possible class
+ *   stats_device          float [rows][2] or NULL: what isr_logprobs_grad reads
+ * Empty row: log-probabilities -infinity, entropy 0.  ISR_ERR_ARG if nothing is asked for. */
+size_t isr_logprobs_workspace_bytes(const isr_logits *logits, uint32_t top);
+int isr_logprobs(const isr_logits *logits, const int32_t *given_device, uint32_t given, uint32_t top,
+                 float *logprob_device, float *entropy_device, int32_t *top_class_device,
+                 float *top_logprob_device, float *stats_device, void *workspace_device,
+                 size_t workspace_bytes, void *hip_stream);
+
+/* Gradient of sum_r (sum_g grad_logprob[r][g] * logprob[r][g] + grad_entropy[r] * entropy[r]) by
+ * the logits: scale (sum_g u_g ([j = c_g] - p_j) - u_H p_j (log p_j + H)).  stats_device and
+ * entropy_device (with grad_entropy_device, else both NULL) as isr_logprobs left them for the
+ * same logits and scale.  To have the gradient of the top alternatives, give them as the given.
+ * A row whose given classes are all negative and whose grad_entropy is absent or 0 gets zeros
+ * whatever it holds; so does an empty row.  grad_logits_device: [rows][grad_row_stride] of the logits'
+ * type (float for int32 logits), columns from `classes` on are left as they are; may be
+ * the logits' own memory, with their stride, and must not overlap it otherwise. */
+int isr_logprobs_grad(const isr_logits *logits, const int32_t *given_device, uint32_t given,
+                      const float *grad_logprob_device, const float *entropy_device,
+                      const float *grad_entropy_device, const float *stats_device,
+                      void *grad_logits_device, uint64_t grad_row_stride, void *hip_stream);
+
+/* Top logits of a teacher: per row `top` entries of a class and a value v = scale * logit; a
+ * negative class is no entry, a class >= classes of the student makes the row's results NaN.
+ *   rest == 0: q = softmax of the entries' v (any common offset is free): the teacher's law on
+ *              its top classes
+ *   rest == 1: v are log-probabilities (isr_logprobs' top_logprob): q_i = exp v_i, and what they
+ *              leave, q_rest = max(0, 1 - sum q_i), belongs to all other classes together */
+typedef struct isr_teacher {
+    const int32_t *class_device; /* [rows][top] */
+    const void *logit_device;    /* [rows][top] */
+    int32_t type;                /* ISR_F32, ISR_BF16 or ISR_F16 */
+    uint32_t top;                /* 1 .. ISR_MAX_GIVEN */
+    float scale;                 /* finite, > 0 */
+    int32_t rest;
+} isr_teacher;
+
+/* loss[r] = sum_i q_i (log q_i - log p_{c_i}) [+ q_rest (log q_rest - log p_rest), p_rest the
+ * student's probability of all classes that are no entry], terms with q = 0 left out.  A row
+ * without an entry (or, rest == 0, with all its values -infinity) has loss 0 and gradient 0 whatever
+ * it holds.  An empty row has gradient 0.  A class named by two entries gets both their q.
+ *   row_weight_device     float [rows] or NULL (1): the gradient's factor, i.e. the gradient by
+ *                         loss[r] of what is trained; 0 gives gradient 0 whatever the row holds
+ *   loss_device           float [rows], without the weight
+ *   stats_device          float [rows][8] or NULL: what isr_distill_grad reads
+ *   grad_logits_device    NULL, or the gradient row_weight[r] * d loss[r] / d x as
+ *                         isr_distill_grad writes it (then stats_device may still be NULL) */
+size_t isr_distill_workspace_bytes(const isr_logits *student, const isr_teacher *teacher);
+int isr_distill(const isr_logits *student, const isr_teacher *teacher, const float *row_weight_device,
+                float *loss_device, float *stats_device, void *grad_logits_device,
+                uint64_t grad_row_stride, void *workspace_device, size_t workspace_bytes, void *hip_stream);
+/* The gradient alone, from the statistics of an earlier call with the same student and teacher.
+ * grad_logits_device as in isr_logprobs_grad. */
+int isr_distill_grad(const isr_logits *student, const isr_teacher *teacher, const float *row_weight_device,
+                     const float *stats_device, void *grad_logits_device, uint64_t grad_row_stride,
+                     void *hip_stream);
+
 /* ---- the paper's floating-point comparison systems ------------------------- */
 
 /* Section "Experiments" compares integer randomized smoothing with standard randomized smoothing

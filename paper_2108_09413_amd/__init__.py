@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -27,6 +28,8 @@ EXPORTS = [
     "isr_noise_bank_static", "isr_noise_bank_static_capacity",
     "isr_float_workspace_bytes", "isr_float_chunk", "isr_float_certify", "isr_float_debug_noisy",
     "isr_float_debug_forward", "isr_float_debug_tensor",
+    "isr_logprobs_workspace_bytes", "isr_logprobs", "isr_logprobs_grad",
+    "isr_distill_workspace_bytes", "isr_distill", "isr_distill_grad",
 ]
 
 FLOATRS_QUANT, FLOATRS_FP = 1, 2   # the paper's two floating-point comparison systems
@@ -54,6 +57,16 @@ class Result(C.Structure):
 
 class Item(C.Structure):
     _fields_ = [("image", C.c_uint32), ("sigma", C.c_uint32), ("image_id", C.c_uint32)]
+
+
+class Logits(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("classes", C.c_uint32), ("rows", C.c_uint64),
+                ("row_stride", C.c_uint64), ("scale", C.c_float)]
+
+
+class Teacher(C.Structure):
+    _fields_ = [("cls", C.c_void_p), ("logit", C.c_void_p), ("type", C.c_int32), ("top", C.c_uint32),
+                ("scale", C.c_float), ("rest", C.c_int32)]
 
 
 class KernelStat(C.Structure):
@@ -109,6 +122,15 @@ def lib():
         L.isr_float_debug_noisy.argtypes = [vp, vp, flt, u64, u32, u32, u32, u32, C.c_int, vp]
         L.isr_float_debug_forward.argtypes = [vp, vp, flt, u64, u32, u32, u32, u32, C.c_int, vp, vp, vp]
         L.isr_float_debug_tensor.argtypes = [vp, vp, flt, u64, u32, u32, u32, i32, vp]
+        pl, pt = C.POINTER(Logits), C.POINTER(Teacher)
+        L.isr_logprobs_workspace_bytes.argtypes = [pl, u32]
+        L.isr_logprobs_workspace_bytes.restype = sz
+        L.isr_logprobs.argtypes = [pl, vp, u32, u32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.isr_logprobs_grad.argtypes = [pl, vp, u32, vp, vp, vp, vp, vp, u64, vp]
+        L.isr_distill_workspace_bytes.argtypes = [pl, pt]
+        L.isr_distill_workspace_bytes.restype = sz
+        L.isr_distill.argtypes = [pl, pt, vp, vp, vp, vp, u64, vp, sz, vp]
+        L.isr_distill_grad.argtypes = [pl, pt, vp, vp, vp, u64, vp]
         L.isr_set_fusion.argtypes = [vp, C.c_int]
         L.isr_set_conv_tile.argtypes = [vp, C.c_int]
         L.isr_profile.argtypes = [vp, u32]
@@ -118,7 +140,8 @@ def lib():
         L.isr_last_device_error.argtypes = []
         for name in EXPORTS:
             if name not in ("isr_workspace_bytes", "isr_strerror", "isr_noise_bank_static_capacity",
-                            "isr_float_workspace_bytes", "isr_float_chunk"):
+                            "isr_float_workspace_bytes", "isr_float_chunk", "isr_logprobs_workspace_bytes",
+                            "isr_distill_workspace_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -426,6 +449,168 @@ def isr_float_debug_tensor(model: Model, x, sigma: float, seed: int, image_id: i
     out = np.zeros(shape, dtype=np.float32)
     _check(lib().isr_float_debug_tensor(model.handle, C.c_void_p(x.data_ptr()), C.c_float(sigma), C.c_uint64(seed), image_id,
                                         phase, sample, tensor_id, _np_ptr(out)), "isr_float_debug_tensor")
+    return out
+
+
+# ---- operators on rows of class logits -----------------------------------------
+
+F32, BF16, F16, I32 = range(4)   # element types
+
+
+class LogProbs(NamedTuple):
+    given: object      # float32 [rows, given], None without given classes
+    entropy: object    # float32 [rows]
+    top_class: object  # int32 [rows, top]
+    top: object        # float32 [rows, top]
+    stats: object      # float32 [rows, 2], for isr_logprobs_grad
+
+
+class Distilled(NamedTuple):
+    loss: object       # float32 [rows]
+    stats: object      # float32 [rows, 8], for isr_distill_grad
+    grad: object       # [rows, classes] of the logits' type
+
+
+def _types():
+    import torch
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32}
+
+
+def _refuse(why: str):
+    raise IsrError(ISR_ERR_ARG, why)
+
+
+def _logits(x, scale: float) -> Logits:
+    kind = _types().get(x.dtype)
+    if kind is None:
+        _refuse(f"logits of type {x.dtype}")
+    if not x.is_cuda or x.dim() != 2:
+        _refuse("logits are a [rows, classes] tensor on the device")
+    rows, classes = x.shape
+    if classes == 0 or (classes > 1 and rows and x.stride(1) != 1):
+        _refuse(f"logits of shape {tuple(x.shape)}, strides {x.stride()}")
+    return Logits(x.data_ptr(), kind, classes, rows, x.stride(0) if rows > 1 else classes, scale)
+
+
+def _operand(t, shape, dtypes, x, what: str):
+    """Pointer of a contiguous tensor on the logits' device (None: null), checked."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or t.device != x.device or not t.is_contiguous():
+        _refuse(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device} beside logits {tuple(x.shape)} on {x.device}")
+    return t.data_ptr()
+
+
+def _on_device_of(x, call):
+    """Runs call(stream) with the logits' device current."""
+    import torch
+    if x.device.index == torch.cuda.current_device():
+        return call(torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(x.device):
+        return call(torch.cuda.current_stream().cuda_stream)
+
+
+def _workspace(x, need: int):
+    import torch
+    return torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+
+
+def _grad_rows(x, out):
+    """The tensor that the gradient goes to and its row stride."""
+    import torch
+    dtype = torch.float32 if x.dtype == torch.int32 else x.dtype
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    elif out.dtype != dtype or out.shape != x.shape or out.device != x.device or (x.shape[1] > 1 and x.shape[0] and out.stride(1) != 1):
+        _refuse(f"gradient {out.dtype} {tuple(out.shape)} of logits {x.dtype} {tuple(x.shape)}")
+    return out, out.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def isr_logprobs(logits, given=None, top: int = 0, entropy: bool = False, scale: float = 1.0, stats: bool = False) -> LogProbs:
+    """Log-probabilities of the given classes (int32 [rows, given], negative: does not count), entropy and top alternatives
+    of rows of logits, on the current stream of their device."""
+    import torch
+    l = _logits(logits, scale)
+    rows, f32 = l.rows, torch.float32
+    n = 0
+    if given is not None:
+        if given.dim() != 2:
+            _refuse("given classes are [rows, given]")
+        n = given.shape[1]
+    pg = _operand(given, (rows, n), (torch.int32,), logits, "given classes")
+
+    def new(*shape, dtype=f32):
+        return torch.empty(shape, dtype=dtype, device=logits.device)
+    r = LogProbs(new(rows, n) if n else None, new(rows) if entropy else None, new(rows, top, dtype=torch.int32) if top > 0 else None,
+                 new(rows, top) if top > 0 else None, new(rows, 2) if stats else None)
+    need = lib().isr_logprobs_workspace_bytes(C.byref(l), max(top, 0))
+    ws = _workspace(logits, need)
+    p = [t.data_ptr() if t is not None else None for t in r]
+    _check(_on_device_of(logits, lambda st: lib().isr_logprobs(C.byref(l), pg, n, top if top >= 0 else ~0 & 0xFFFFFFFF, *p,
+                                                               ws.data_ptr() if need else None, need, st)), "isr_logprobs")
+    return r
+
+
+def isr_logprobs_grad(logits, given, grad_logprob, stats, entropy=None, grad_entropy=None, scale: float = 1.0, out=None):
+    """Gradient by the logits of sum(grad_logprob * r.given) + sum(grad_entropy * r.entropy), r = isr_logprobs(logits, given,
+    stats=True, ...).  out: where it goes; may be the logits themselves."""
+    import torch
+    l = _logits(logits, scale)
+    f32 = (torch.float32,)
+    n = 0
+    if given is not None:
+        if given.dim() != 2:
+            _refuse("given classes are [rows, given]")
+        n = given.shape[1]
+    p = [_operand(given, (l.rows, n), (torch.int32,), logits, "given classes"), n,
+         _operand(grad_logprob, (l.rows, n), f32, logits, "gradient of the log-probabilities"),
+         _operand(entropy, (l.rows,), f32, logits, "entropy"), _operand(grad_entropy, (l.rows,), f32, logits, "gradient of the entropy"),
+         _operand(stats, (l.rows, 2), f32, logits, "statistics")]
+    out, stride = _grad_rows(logits, out)
+    _check(_on_device_of(logits, lambda st: lib().isr_logprobs_grad(C.byref(l), *p, out.data_ptr(), stride, st)), "isr_logprobs_grad")
+    return out
+
+
+def _teacher(x, l, entry, value, scale, rest):
+    import torch
+    if entry.dim() != 2:
+        _refuse("the teacher's classes are [rows, top]")
+    shape = (l.rows, entry.shape[1])
+    pe = _operand(entry, shape, (torch.int32,), x, "the teacher's classes")
+    pv = _operand(value, shape, (torch.float32, torch.bfloat16, torch.float16), x, "the teacher's logits")
+    return Teacher(pe, pv, _types()[value.dtype], shape[1], scale, int(bool(rest)))
+
+
+def isr_distill(logits, teacher_class, teacher_logit, weight=None, rest: bool = False, scale: float = 1.0,
+                teacher_scale: float = 1.0, grad=False, stats: bool = False) -> Distilled:
+    """Distillation loss of each row from a teacher's top logits (int32 and float [rows, top]; negative class: no entry).
+    weight (float32 [rows]): the gradient's factor.  grad: True, or the tensor it goes to (may be the logits themselves)."""
+    import torch
+    l = _logits(logits, scale)
+    t = _teacher(logits, l, teacher_class, teacher_logit, teacher_scale, rest)
+    pw = _operand(weight, (l.rows,), (torch.float32,), logits, "weights")
+    loss = torch.empty(l.rows, dtype=torch.float32, device=logits.device)
+    st8 = torch.empty((l.rows, 8), dtype=torch.float32, device=logits.device) if stats else None
+    out, stride = (None, 0) if grad is None or grad is False else _grad_rows(logits, None if grad is True else grad)
+    need = lib().isr_distill_workspace_bytes(C.byref(l), C.byref(t))
+    ws = _workspace(logits, need)
+    _check(_on_device_of(logits, lambda st: lib().isr_distill(C.byref(l), C.byref(t), pw, loss.data_ptr(), st8.data_ptr() if stats else None,
+                                                              out.data_ptr() if out is not None else None, stride,
+                                                              ws.data_ptr() if need else None, need, st)), "isr_distill")
+    return Distilled(loss, st8, out)
+
+
+def isr_distill_grad(logits, teacher_class, teacher_logit, stats, weight=None, rest: bool = False, scale: float = 1.0,
+                     teacher_scale: float = 1.0, out=None):
+    """The gradient of isr_distill alone, from the statistics of that call."""
+    import torch
+    l = _logits(logits, scale)
+    t = _teacher(logits, l, teacher_class, teacher_logit, teacher_scale, rest)
+    f32 = (torch.float32,)
+    pw, ps = _operand(weight, (l.rows,), f32, logits, "weights"), _operand(stats, (l.rows, 8), f32, logits, "statistics")
+    out, stride = _grad_rows(logits, out)
+    _check(_on_device_of(logits, lambda st: lib().isr_distill_grad(C.byref(l), C.byref(t), pw, ps, out.data_ptr(), stride, st)),
+           "isr_distill_grad")
     return out
 
 

@@ -1,0 +1,138 @@
+// Entry points of the operators on rows of class logits: arguments are checked here, on the host, and the kernels
+// rely on it.  Nothing is allocated, copied or waited for.
+#include <cmath>
+
+#include "logit_rows.h"
+
+namespace {
+
+using namespace isr;
+
+constexpr uint32_t MAX_CLASSES = 1u << 24;
+constexpr size_t DISTILL_STATS = 8 * sizeof(float);
+
+size_t element_bytes(int type) { return type == ISR_F32 || type == ISR_I32 ? 4 : 2; }
+bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
+bool usable_scale(float s) { return std::isfinite(s) && s > 0.f; }
+
+// shapes and type, what the size of a workspace depends on
+bool valid_shape(const isr_logits *l) {
+    return l && l->type >= ISR_F32 && l->type <= ISR_I32 && l->classes >= 1 && l->classes <= MAX_CLASSES && l->rows <= 0x7FFFFFFF;
+}
+
+// elements that rows of a stride span, 0 where that passes 2^60
+uint64_t span(uint64_t rows, uint64_t stride, uint32_t classes) {
+    if (rows == 0) return 0;
+    if (rows > 1 && stride > ((1ull << 60) - classes) / (rows - 1)) return 0;
+    return (rows - 1) * stride + classes;
+}
+
+bool valid_logits(const isr_logits *l) {
+    if (!valid_shape(l) || !usable_scale(l->scale) || l->row_stride < l->classes) return false;
+    return l->rows == 0 || (l->data_device && aligned(l->data_device, element_bytes(l->type)) && span(l->rows, l->row_stride, l->classes));
+}
+
+bool valid_teacher(const isr_teacher *t) {
+    return t && t->type >= ISR_F32 && t->type <= ISR_F16 && t->top >= 1 && t->top <= ISR_MAX_GIVEN && usable_scale(t->scale) &&
+           (t->rest == 0 || t->rest == 1);
+}
+
+bool teacher_data(const isr_teacher *t) {
+    return t->class_device && t->logit_device && aligned(t->class_device, 4) && aligned(t->logit_device, element_bytes(t->type));
+}
+
+// a gradient's rows: their own memory, or the logits' with the logits' type and stride
+bool valid_grad(const isr_logits *l, const void *grad, uint64_t stride) {
+    const size_t bytes = l->type == ISR_I32 ? 4 : element_bytes(l->type);
+    if (!grad || !aligned(grad, bytes) || stride < l->classes || !span(l->rows, stride, l->classes)) return false;
+    if (grad == l->data_device) return stride == l->row_stride && l->type != ISR_I32;
+    const uintptr_t g = (uintptr_t)grad, x = (uintptr_t)l->data_device;
+    const uint64_t gb = span(l->rows, stride, l->classes) * bytes, xb = span(l->rows, l->row_stride, l->classes) * element_bytes(l->type);
+    return g >= x ? g - x >= xb : x - g >= gb;
+}
+
+bool all_aligned(std::initializer_list<const void *> words) {
+    for (const void *p : words)
+        if (!aligned(p, 4)) return false;
+    return true;
+}
+
+LogitRows rows_of(const isr_logits *l) { return {l->data_device, l->type, l->classes, l->rows, l->row_stride, l->scale}; }
+
+DistillParams distill_params(const isr_logits *l, const isr_teacher *t, const float *weight, float *loss, float *stats, void *grad,
+                             uint64_t grad_stride) {
+    return {rows_of(l), t->class_device, t->logit_device, t->type, t->top, t->scale, t->rest, weight, loss, stats, grad, grad_stride};
+}
+
+int status(hipError_t e) {
+    if (e == hipSuccess) return ISR_OK;
+    set_last_device_error((int)e);
+    return ISR_ERR_DEVICE;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t isr_logprobs_workspace_bytes(const isr_logits *, uint32_t) { return 0; }
+
+int isr_logprobs(const isr_logits *l, const int32_t *given_device, uint32_t given, uint32_t top, float *logprob_device,
+                 float *entropy_device, int32_t *top_class_device, float *top_logprob_device, float *stats_device,
+                 void *workspace_device, size_t workspace_bytes, void *hip_stream) {
+    if (!valid_logits(l) || given > ISR_MAX_GIVEN || top > ISR_MAX_TOP || top > l->classes) return ISR_ERR_ARG;
+    if (!given && !top && !entropy_device && !stats_device) return ISR_ERR_ARG;
+    if (l->rows == 0) return ISR_OK;
+    if (given && (!given_device || !logprob_device)) return ISR_ERR_ARG;
+    if (top && (!top_class_device || !top_logprob_device)) return ISR_ERR_ARG;
+    if (!all_aligned({given_device, logprob_device, entropy_device, top_class_device, top_logprob_device, stats_device})) return ISR_ERR_ARG;
+    if (workspace_bytes < isr_logprobs_workspace_bytes(l, top)) return ISR_ERR_WORKSPACE;
+    (void)workspace_device;
+    return status(launch_logprobs({rows_of(l), given_device, given, top, logprob_device, entropy_device, top_class_device, top_logprob_device, stats_device},
+                                  (hipStream_t)hip_stream));
+}
+
+int isr_logprobs_grad(const isr_logits *l, const int32_t *given_device, uint32_t given, const float *grad_logprob_device,
+                      const float *entropy_device, const float *grad_entropy_device, const float *stats_device,
+                      void *grad_logits_device, uint64_t grad_row_stride, void *hip_stream) {
+    if (!valid_logits(l) || given > ISR_MAX_GIVEN) return ISR_ERR_ARG;
+    if (!given && !grad_entropy_device) return ISR_ERR_ARG;
+    if (!entropy_device != !grad_entropy_device) return ISR_ERR_ARG;
+    if (l->rows == 0) return ISR_OK;
+    if (given && (!given_device || !grad_logprob_device)) return ISR_ERR_ARG;
+    if (!stats_device || !all_aligned({given_device, grad_logprob_device, entropy_device, grad_entropy_device, stats_device})) return ISR_ERR_ARG;
+    if (!valid_grad(l, grad_logits_device, grad_row_stride)) return ISR_ERR_ARG;
+    return status(launch_logprobs_grad({rows_of(l), given_device, given, grad_logprob_device, entropy_device, grad_entropy_device, stats_device,
+                                        grad_logits_device, grad_row_stride}, (hipStream_t)hip_stream));
+}
+
+// one row's statistics when the caller keeps none: the gradient's kernel reads them
+size_t isr_distill_workspace_bytes(const isr_logits *l, const isr_teacher *t) {
+    if (!valid_shape(l) || !valid_teacher(t)) return 0;
+    return l->rows * DISTILL_STATS;
+}
+
+int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weight_device, float *loss_device, float *stats_device,
+                void *grad_logits_device, uint64_t grad_row_stride, void *workspace_device, size_t workspace_bytes, void *hip_stream) {
+    if (!valid_logits(l) || !valid_teacher(t)) return ISR_ERR_ARG;
+    if (l->rows == 0) return ISR_OK;
+    if (!teacher_data(t) || !loss_device || !all_aligned({row_weight_device, loss_device, stats_device})) return ISR_ERR_ARG;
+    if (grad_logits_device && !valid_grad(l, grad_logits_device, grad_row_stride)) return ISR_ERR_ARG;
+    if (!workspace_device || workspace_bytes < isr_distill_workspace_bytes(l, t)) return ISR_ERR_WORKSPACE;
+    if (!aligned(workspace_device, 16)) return ISR_ERR_ARG;
+    DistillParams p = distill_params(l, t, row_weight_device, loss_device, stats_device ? stats_device : (float *)workspace_device, grad_logits_device, grad_row_stride);
+    hipError_t e = launch_distill(p, (hipStream_t)hip_stream);
+    if (e == hipSuccess && grad_logits_device) e = launch_distill_grad(p, (hipStream_t)hip_stream);
+    return status(e);
+}
+
+int isr_distill_grad(const isr_logits *l, const isr_teacher *t, const float *row_weight_device, const float *stats_device,
+                     void *grad_logits_device, uint64_t grad_row_stride, void *hip_stream) {
+    if (!valid_logits(l) || !valid_teacher(t)) return ISR_ERR_ARG;
+    if (l->rows == 0) return ISR_OK;
+    if (!teacher_data(t) || !stats_device || !all_aligned({row_weight_device, stats_device})) return ISR_ERR_ARG;
+    if (!valid_grad(l, grad_logits_device, grad_row_stride)) return ISR_ERR_ARG;
+    return status(launch_distill_grad(distill_params(l, t, row_weight_device, nullptr, const_cast<float *>(stats_device), grad_logits_device, grad_row_stride),
+                                      (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

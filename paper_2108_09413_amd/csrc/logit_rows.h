@@ -1,0 +1,52 @@
+// Operators on rows of class logits: what their entry points (logit_api.cpp) hand to their kernels (logit_rows.hip).
+#pragma once
+#include "isr_internal.h"
+
+namespace isr {
+
+struct LogitRows {
+    const void *x;
+    int32_t type;
+    uint32_t classes;
+    uint64_t rows, stride;
+    float scale;
+};
+
+struct LogprobsParams {
+    LogitRows l;
+    const int32_t *given;
+    uint32_t n_given, top;
+    float *logprob, *entropy;
+    int32_t *top_class;
+    float *top_logprob, *stats;
+};
+
+struct LogprobsGradParams {
+    LogitRows l;
+    const int32_t *given;
+    uint32_t n_given;
+    const float *up_logprob, *entropy, *up_entropy, *stats;
+    void *grad;
+    uint64_t grad_stride;
+};
+
+struct DistillParams {
+    LogitRows l;
+    const int32_t *entry;
+    const void *value;
+    int32_t value_type;
+    uint32_t top;
+    float value_scale;
+    int32_t rest;
+    const float *weight;
+    float *loss, *stats;      // stats: [rows][8], DistillStat
+    void *grad;
+    uint64_t grad_stride;
+};
+
+hipError_t launch_logprobs(const LogprobsParams &p, hipStream_t st);
+hipError_t launch_logprobs_grad(const LogprobsGradParams &p, hipStream_t st);
+hipError_t launch_distill(const DistillParams &p, hipStream_t st);
+hipError_t launch_distill_grad(const DistillParams &p, hipStream_t st);
+
+}  // namespace isr
