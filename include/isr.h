@@ -184,7 +184,7 @@ size_t isr_noise_bank_static_capacity(void);
  * top logits of another, e.g. the int8 network's on the fp32 network's.  Both work on logits in
  * device memory, are enqueued on hip_stream (NULL = default; of the current device, which is the
  * one that holds the memory) and return at once: no allocation, no copy, no synchronisation, so
- * a call can be captured into a graph.  Workspaces hold nothing between calls; calls that may
+ * a call can be captured into a graph.  Workspaces (aligned to 16 bytes) hold nothing between calls; calls that may
  * overlap in time need a workspace each.  Results do not depend on the order in which workgroups
  * run.  Sums and statistics are fp32 or wider.
  *

@@ -74,7 +74,11 @@ int status(hipError_t e) {
 
 extern "C" {
 
-size_t isr_logprobs_workspace_bytes(const isr_logits *, uint32_t) { return 0; }
+size_t isr_logprobs_workspace_bytes(const isr_logits *l, uint32_t top) {
+    if (!valid_shape(l) || l->rows == 0 || top > ISR_MAX_TOP) return 0;
+    const RowCut cut = cut_rows(l->type, l->classes, l->rows, top);
+    return cut.parts_bytes + cut.lists_bytes;
+}
 
 int isr_logprobs(const isr_logits *l, const int32_t *given_device, uint32_t given, uint32_t top, float *logprob_device,
                  float *entropy_device, int32_t *top_class_device, float *top_logprob_device, float *stats_device,
@@ -85,10 +89,15 @@ int isr_logprobs(const isr_logits *l, const int32_t *given_device, uint32_t give
     if (given && (!given_device || !logprob_device)) return ISR_ERR_ARG;
     if (top && (!top_class_device || !top_logprob_device)) return ISR_ERR_ARG;
     if (!all_aligned({given_device, logprob_device, entropy_device, top_class_device, top_logprob_device, stats_device})) return ISR_ERR_ARG;
-    if (workspace_bytes < isr_logprobs_workspace_bytes(l, top)) return ISR_ERR_WORKSPACE;
-    (void)workspace_device;
-    return status(launch_logprobs({rows_of(l), given_device, given, top, logprob_device, entropy_device, top_class_device, top_logprob_device, stats_device},
-                                  (hipStream_t)hip_stream));
+    const RowCut cut = cut_rows(l->type, l->classes, l->rows, top);
+    const size_t need = cut.parts_bytes + cut.lists_bytes;
+    if (need && (!workspace_device || workspace_bytes < need)) return ISR_ERR_WORKSPACE;
+    if (need && !aligned(workspace_device, 16)) return ISR_ERR_ARG;
+    LogprobsParams p{};
+    p.l = rows_of(l);
+    p.given = given_device; p.n_given = given; p.top = top;
+    p.logprob = logprob_device; p.entropy = entropy_device; p.top_class = top_class_device; p.top_logprob = top_logprob_device; p.stats = stats_device;
+    return status(launch_logprobs(p, cut, workspace_device, (hipStream_t)hip_stream));
 }
 
 int isr_logprobs_grad(const isr_logits *l, const int32_t *given_device, uint32_t given, const float *grad_logprob_device,

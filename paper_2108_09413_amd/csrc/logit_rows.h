@@ -12,6 +12,18 @@ struct LogitRows {
     float scale;
 };
 
+// How rows are cut into chunks of a workgroup each (cut_rows), and what the chunks need of the workspace.
+struct RowCut {
+    uint32_t nv;           // vectors of 16 bytes a thread
+    uint32_t chunks;       // of a row
+    uint32_t chunk_vecs;   // vectors of a chunk, the last one's may be fewer
+    uint32_t list_cap;     // room for candidates of the top alternatives, of a chunk
+    uint32_t rows;         // of a launch
+    size_t parts_bytes, lists_bytes;
+};
+RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top);
+
+struct Part;
 struct LogprobsParams {
     LogitRows l;
     const int32_t *given;
@@ -19,6 +31,11 @@ struct LogprobsParams {
     float *logprob, *entropy;
     int32_t *top_class;
     float *top_logprob, *stats;
+    // set by the launcher
+    uint64_t row0;
+    uint32_t chunks, chunk_vecs, list_cap;
+    Part *parts;
+    uint2 *lists;
 };
 
 struct LogprobsGradParams {
@@ -44,7 +61,7 @@ struct DistillParams {
     uint64_t grad_stride;
 };
 
-hipError_t launch_logprobs(const LogprobsParams &p, hipStream_t st);
+hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st);
 hipError_t launch_logprobs_grad(const LogprobsGradParams &p, hipStream_t st);
 hipError_t launch_distill(const DistillParams &p, hipStream_t st);
 hipError_t launch_distill_grad(const DistillParams &p, hipStream_t st);

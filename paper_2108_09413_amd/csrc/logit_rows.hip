@@ -1,11 +1,16 @@
 // Operators on rows of class logits: log-probabilities of given classes with entropy and top alternatives, distillation from
 // a teacher's top logits, and the gradient of both.
 //
-// Row statistics: m = max x, s = sum exp(scale (x - m)), t = sum exp(.) scale (x - m).  Differences are taken before
-// the scale, so rows of the type's lowest value, far offsets and int32 logits (whose differences are exact) lose nothing.
-// s is NaN exactly for rows that hold NaN or +infinity, m is -infinity for rows without a possible class.
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
+// Statistics of a set of logits: m = max x, s = sum exp(scale (x - m)), t = sum exp(.) * (scale (x - m) log2 e).  Differences
+// are taken before the scale, so rows of the type's lowest value, far offsets and int32 logits (whose differences are exact)
+// lose nothing.  s is NaN exactly for rows that hold NaN or +infinity, m is -infinity for rows without a possible class.
+//
+// Forward: a row is cut into chunks of up to 256 * NV vectors of 16 bytes, one workgroup each, which holds its chunk in
+// registers: one pass over memory, then maximum, exponentials and candidates of the top alternatives from registers.  The
+// chunks' results meet in a second launch (join), or in the same one where a row is one chunk.
+// Gradient: element by element from the row's statistics; the few classes that are named (given, or entries of the teacher)
+// are overwritten behind a barrier by one thread each.
+#include <algorithm>
 
 #include "logit_rows.h"
 
@@ -16,17 +21,17 @@ constexpr float NEG_INF = -__builtin_inff();
 template <int TYPE> struct Kind;
 template <> struct Kind<ISR_F32> {
     using Raw = float; using Val = float; using Grad = float;
-    static __device__ __forceinline__ float val(float r) { return r + 0.f; }   // -0 and 0 are one value
+    static __device__ __forceinline__ float val(float r) { return r; }
     static __device__ __forceinline__ float grad(float g) { return g; }
 };
 template <> struct Kind<ISR_BF16> {
-    using Raw = uint16_t; using Val = float; using Grad = __hip_bfloat16;
-    static __device__ __forceinline__ float val(uint16_t r) { return __uint_as_float((uint32_t)r << 16) + 0.f; }
-    static __device__ __forceinline__ __hip_bfloat16 grad(float g) { return __float2bfloat16(g); }   // the caller's type: one rounding, to nearest
+    using Raw = uint16_t; using Val = float; using Grad = __bf16;
+    static __device__ __forceinline__ float val(uint16_t r) { return __uint_as_float((uint32_t)r << 16); }
+    static __device__ __forceinline__ __bf16 grad(float g) { return (__bf16)g; }   // the caller's type: one rounding, to nearest
 };
 template <> struct Kind<ISR_F16> {
     using Raw = _Float16; using Val = float; using Grad = _Float16;
-    static __device__ __forceinline__ float val(_Float16 r) { return (float)r + 0.f; }
+    static __device__ __forceinline__ float val(_Float16 r) { return (float)r; }
     static __device__ __forceinline__ _Float16 grad(float g) { return (_Float16)g; }
 };
 template <> struct Kind<ISR_I32> {
@@ -37,7 +42,7 @@ template <> struct Kind<ISR_I32> {
 
 __device__ __forceinline__ float lowest(float) { return NEG_INF; }
 __device__ __forceinline__ int32_t lowest(int32_t) { return INT32_MIN; }
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // NaN stays
 __device__ __forceinline__ int32_t larger(int32_t a, int32_t b) { return a > b ? a : b; }
 // x - m, m >= x; no possible class at all: x itself, which is -infinity
 __device__ __forceinline__ float below(float x, float m) { return x - (m == NEG_INF ? 0.f : m); }
@@ -52,12 +57,369 @@ template <class Val> __device__ __forceinline__ Val of_bits(float b);
 template <> __device__ __forceinline__ float of_bits<float>(float b) { return b; }
 template <> __device__ __forceinline__ int32_t of_bits<int32_t>(float b) { return __float_as_int(b); }
 
+
+constexpr int THREADS = 256;
+constexpr int LIST = 512;                 // candidates of the top alternatives in LDS
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NO_SHARE = -200.f;        // 2^-200 is 0 in fp32: finite in place of log2 0, so that 0 * log 0 is 0
+
+// ---- across a wave, across a workgroup ------------------------------------------
+
+template <int CTRL> __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true); }
+template <class T, class Op>
+__device__ __forceinline__ T wave_fold(T v, Op op) {   // of all 64 lanes, in every lane
+    auto as = [](int b) { return __builtin_bit_cast(T, b); };
+    auto bits = [](T x) { return __builtin_bit_cast(int, x); };
+    v = op(v, as(dpp<0xB1>(bits(v))));    // lane ^ 1
+    v = op(v, as(dpp<0x4E>(bits(v))));    // lane ^ 2
+    v = op(v, as(dpp<0x141>(bits(v))));   // the other half of eight
+    v = op(v, as(dpp<0x140>(bits(v))));   // the other half of sixteen
+    auto at = [&](int lane) { return as(__builtin_amdgcn_readlane(bits(v), lane)); };
+    return op(op(at(0), at(16)), op(at(32), at(48)));
+}
+__device__ __forceinline__ float wave_sum(float v) { return wave_fold(v, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ int wave_sum(int v) { return wave_fold(v, [](int a, int b) { return a + b; }); }
+template <class T> __device__ __forceinline__ T wave_max(T v) { return wave_fold(v, [](T a, T b) { return larger(a, b); }); }
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
 template <class Val>
 struct Stat {
     Val m;
     float s, t;
+};
+
+struct Shared {
+    uint32_t key[THREADS];      // largest key of each thread
+    uint2 list[LIST + 2];       // candidates: (key, ~class), so that the larger 64-bit number comes first
+    uint32_t m[THREADS / 64];   // Val
+    float s[THREADS / 64], t[THREADS / 64];
+    int count[THREADS / 64];
+    uint32_t listed;
+};
+
+// The workgroup's statistics from those of its threads.  Two barriers; `with_keys` has something stored before the first.
+template <class Val, class Between>
+__device__ __forceinline__ Stat<Val> block_stat(Stat<Val> a, float c, Shared &sh, Between with_keys) {
+    const int wave = threadIdx.x >> 6;
+    const Val wm = wave_max(a.m);
+    if ((threadIdx.x & 63) == 0) sh.m[wave] = __builtin_bit_cast(uint32_t, wm);
+    with_keys();
+    __syncthreads();
+    Val m = __builtin_bit_cast(Val, sh.m[0]);
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) m = larger(m, __builtin_bit_cast(Val, sh.m[w]));
+    const float d = c * below(a.m, m), f = __builtin_amdgcn_exp2f(d);
+    const float s = a.s == 0.f ? 0.f : f * a.s, t = a.s == 0.f ? 0.f : f * (a.t + fmaxf(d, NO_SHARE) * a.s);
+    const float ws = wave_sum(s), wt = wave_sum(t);
+    if ((threadIdx.x & 63) == 0) { sh.s[wave] = ws; sh.t[wave] = wt; }
+    __syncthreads();
+    return {m, (sh.s[0] + sh.s[1]) + (sh.s[2] + sh.s[3]), (sh.t[0] + sh.t[1]) + (sh.t[2] + sh.t[3])};
+}
+
+// ---- top alternatives ---------------------------------------------------------------
+// Logits as unsigned keys in the same order (-0 as 0).  The k-th largest of the threads' own maxima, cut to its leading bits,
+// is a bound that k elements at least reach and few more: those are listed, and each finds its place by counting
+// the listed ones in front of it.  Where more are listed than there is room (rows with many equal logits), the exact bound
+// by (key, class) is searched bit by bit and exactly k are listed.
+
+__device__ __forceinline__ uint32_t key_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint32_t key_of(int32_t x) { return (uint32_t)x ^ 0x80000000u; }
+template <class Val> __device__ __forceinline__ Val of_key(uint32_t k);
+template <> __device__ __forceinline__ float of_key<float>(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k); }
+template <> __device__ __forceinline__ int32_t of_key<int32_t>(uint32_t k) { return (int32_t)(k ^ 0x80000000u); }
+template <class Val> __device__ __forceinline__ uint32_t least_key();   // of a possible class
+template <> __device__ __forceinline__ uint32_t least_key<float>() { return 0x00800000u; }
+template <> __device__ __forceinline__ uint32_t least_key<int32_t>() { return 0; }
+template <class Val> constexpr int LOW_BITS = 16;                // fp32 keys: a relative step of 2^-7
+template <> constexpr int LOW_BITS<int32_t> = 0;
+
+// Every wave for itself: the largest bound of leading bits that k of the threads' keys reach, 0 if fewer threads have any.
+// Up to 32 alternatives the threads go by fours.
+template <int LOW>
+__device__ __forceinline__ uint32_t key_bound(const Shared &sh, uint32_t k) {
+    const uint4 q = ((const uint4 *)sh.key)[threadIdx.x & 63];
+    uint32_t bound = 0;
+    if (k <= 32) {
+        const uint32_t top = max(max(q.x, q.y), max(q.z, q.w));
+        for (int b = 31; b >= LOW; --b) {
+            const uint32_t next = bound | (1u << b);
+            if ((uint32_t)__popcll(__ballot(top >= next)) >= k) bound = next;
+        }
+    } else {
+        for (int b = 31; b >= LOW; --b) {
+            const uint32_t next = bound | (1u << b);
+            const int n = __popcll(__ballot(q.x >= next)) + __popcll(__ballot(q.y >= next)) + __popcll(__ballot(q.z >= next)) + __popcll(__ballot(q.w >= next));
+            if ((uint32_t)n >= k) bound = next;
+        }
+    }
+    return bound;
+}
+
+__device__ __forceinline__ int block_count(int n, Shared &sh) {
+    n = wave_sum(n);
+    if ((threadIdx.x & 63) == 0) sh.count[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = (sh.count[0] + sh.count[1]) + (sh.count[2] + sh.count[3]);
+    __syncthreads();
+    return n;
+}
+
+// each(f): f(key, class) for the thread's own possible elements, of which all threads together have more than k.  Lists
+// exactly k.  Returns with the list complete for all threads.
+template <class Each>
+__device__ void list_exactly(Each each, uint32_t k, Shared &sh) {
+    uint32_t hi = 0, lo = 0;
+    bool done = false;
+    for (int b = 31; b >= 0 && !done; --b) {
+        const uint32_t next = hi | (1u << b);
+        int n = 0;
+        each([&](uint32_t key, uint32_t) { n += key >= next; });
+        n = block_count(n, sh);
+        if ((uint32_t)n >= k) { hi = next; done = (uint32_t)n == k; }
+    }
+    if (!done) lo = 0xFF000000u;   // classes are below 2^24
+    for (int b = 23; b >= 0 && !done; --b) {
+        const uint32_t next = lo | (1u << b);
+        int n = 0;
+        each([&](uint32_t key, uint32_t cls) { n += key > hi || (key == hi && ~cls >= next); });
+        n = block_count(n, sh);
+        if ((uint32_t)n >= k) { lo = next; done = (uint32_t)n == k; }
+    }
+    if (threadIdx.x == 0) sh.listed = 0;
+    __syncthreads();
+    each([&](uint32_t key, uint32_t cls) {
+        if (key > hi || (key == hi && ~cls >= lo)) {
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at < LIST) sh.list[at] = make_uint2(key, ~cls);
+        }
+    });
+    __syncthreads();
+}
+
+// ---- rows and their chunks -------------------------------------------------------------
+
+struct __attribute__((packed, aligned(2))) Loose { uint4 v; };   // 16 bytes at any element
+template <int TYPE> constexpr int PER_VEC = 16 / sizeof(typename Kind<TYPE>::Raw);
+
+template <int TYPE>
+__device__ __forceinline__ void unpack(const uint4 &w, typename Kind<TYPE>::Val (&v)[PER_VEC<TYPE>]) {
+    const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (TYPE == ISR_BF16) {
+            v[2 * i] = __uint_as_float(q[i] << 16);
+            v[2 * i + 1] = __uint_as_float(q[i] & 0xFFFF0000u);
+        } else if constexpr (TYPE == ISR_F16) {
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+            const h2 h = __builtin_bit_cast(h2, q[i]);
+            v[2 * i] = (float)h[0];
+            v[2 * i + 1] = (float)h[1];
+        } else {
+            v[i] = __builtin_bit_cast(typename Kind<TYPE>::Val, q[i]);
+        }
+    }
+}
+
+// What a chunk leaves for the join.
+struct Part {
+    uint32_t m;
+    float s, t;
+    uint32_t listed;
+};
+
+// Results of a row of logits, by the whole workgroup.  The list is complete.
+template <int TYPE>
+__device__ void finish_logprobs(const LogprobsParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a, Shared &sh) {
+    using K = Kind<TYPE>;
+    using Val = typename K::Val;
+    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+    const bool bad = a.s != a.s, empty = a.s == 0.f;
+    const float logs = empty ? 0.f : logf(a.s), nan = __builtin_nanf("");
+    auto logp = [&](Val v) { return bad ? nan : possible(v) ? p.l.scale * below(v, a.m) - logs : NEG_INF; };
+    if (threadIdx.x == 0) {
+        if (p.entropy) p.entropy[r] = bad ? nan : empty ? 0.f : logs - LN2 * (a.t / a.s);
+        if (p.stats) { p.stats[2 * r] = bits_of(a.m); p.stats[2 * r + 1] = bad ? nan : empty ? NEG_INF : logs; }
+    }
+    if (threadIdx.x < p.n_given) {
+        const int32_t c = p.given[r * p.n_given + threadIdx.x];
+        p.logprob[r * p.n_given + threadIdx.x] = c < 0 ? 0.f : (uint32_t)c < p.l.classes ? logp(K::val(x[c])) : nan;
+    }
+    if (p.top == 0) return;
+    const uint32_t n = bad ? 0 : min(sh.listed, (uint32_t)LIST);
+    for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
+        const uint2 mine = sh.list[i];
+        const uint64_t own = (uint64_t)mine.x << 32 | mine.y;
+        uint32_t place = 0;
+        for (uint32_t j = 0; j < n; j += 2) {
+            const uint4 two = *(const uint4 *)&sh.list[j];
+            place += ((uint64_t)two.x << 32 | two.y) > own;
+            place += j + 1 < n && ((uint64_t)two.z << 32 | two.w) > own;
+        }
+        if (place < p.top) {
+            p.top_class[r * p.top + place] = (int32_t)~mine.y;
+            p.top_logprob[r * p.top + place] = logp(of_key<Val>(mine.x));
+        }
+    }
+    for (uint32_t k = n + threadIdx.x; k < p.top; k += THREADS) {
+        p.top_class[r * p.top + k] = -1;
+        p.top_logprob[r * p.top + k] = bad ? nan : NEG_INF;
+    }
+}
+
+// A chunk of a row: NV vectors a thread in registers, and what is left behind the row's last vector, an element a thread.
+template <int TYPE, int NV, bool TOP, bool ENT>
+__global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams p) {
+    using K = Kind<TYPE>;
+    using Val = typename K::Val;
+    constexpr int PV = PER_VEC<TYPE>;
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    const uint32_t tid = threadIdx.x, row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks;
+    const uint64_t r = p.row0 + row;
+    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+    const uint32_t vecs = p.l.classes / PV, v0 = chunk * p.chunk_vecs, n = min(p.chunk_vecs, vecs - min(vecs, v0));
+    const uint32_t rest = vecs * PV + tid;
+    const bool tail = chunk == p.chunks - 1 && rest < p.l.classes;   // fewer than PV threads
+    uint4 raw[NV];
+    if (n) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = ((const Loose *)(x + (size_t)(v0 + min(i * THREADS + tid, n - 1)) * PV))->v;
+    }
+    const Val edge = tail ? K::val(x[rest]) : lowest(Val());
+    Stat<Val> a{edge, 0.f, 0.f};
+    if (TOP && tid == 0) sh.listed = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * THREADS + tid >= n) continue;
+        Val v[PV];
+        unpack<TYPE>(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < PV; ++e) a.m = larger(a.m, v[e]);
+    }
+    const float c = p.l.scale * LOG2E;
+    auto add = [&](Val v) {
+        const float d = c * below(v, a.m), e = __builtin_amdgcn_exp2f(d);
+        a.s += e;
+        if (ENT) a.t += e * fmaxf(d, NO_SHARE);
+    };
+    if (tail) add(edge);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * THREADS + tid >= n) continue;
+        Val v[PV];
+        unpack<TYPE>(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < PV; ++e) add(v[e]);
+    }
+    const Stat<Val> all = block_stat(a, c, sh, [&] { if (TOP) sh.key[tid] = key_of(a.m); });
+    if constexpr (TOP) {
+        const uint32_t bound = key_bound<LOW_BITS<Val>>(sh, p.top);
+        const Val from = of_key<Val>(max(bound, least_key<Val>()));
+        auto take = [&](Val v, uint32_t cls) {
+            if (v >= from) {
+                const uint32_t at = atomicAdd(&sh.listed, 1u);
+                if (at < LIST) sh.list[at] = make_uint2(key_of(v), ~cls);
+            }
+        };
+        if (a.m >= from) {
+            if (tail) take(edge, rest);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (i * THREADS + tid >= n) continue;
+                Val v[PV];
+                unpack<TYPE>(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < PV; ++e) take(v[e], (v0 + i * THREADS + tid) * PV + e);
+            }
+        }
+        __syncthreads();
+        if (sh.listed > p.list_cap) {   // uniform; from memory again, an element at a time
+            const uint32_t first = min(v0, vecs) * PV, last = chunk == p.chunks - 1 ? p.l.classes : first + n * PV;
+            __syncthreads();
+            list_exactly([&](auto f) {
+                for (uint32_t j = first + tid; j < last; j += THREADS) {
+                    const Val v = K::val(x[j]);
+                    if (possible(v)) f(key_of(v), j);
+                }
+            }, p.top, sh);
+        }
+    }
+    if (p.chunks == 1) {
+        finish_logprobs<TYPE>(p, r, all, sh);
+        return;
+    }
+    const size_t at = (size_t)row * p.chunks + chunk;
+    if (tid == 0) p.parts[at] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, all.t, TOP ? sh.listed : 0};
+    if constexpr (TOP)
+        for (uint32_t i = tid; i < sh.listed; i += THREADS) p.lists[at * p.list_cap + i] = sh.list[i];
+}
+
+// The chunks of a row together.
+template <class Val>
+__device__ __forceinline__ Stat<Val> join_parts(const Part *parts, uint32_t chunks, float c, Shared &sh) {
+    Stat<Val> a{lowest(Val()), 0.f, 0.f};
+    for (uint32_t i = threadIdx.x; i < chunks; i += THREADS) {
+        const Part q = parts[i];
+        const Val qm = __builtin_bit_cast(Val, q.m), m = larger(a.m, qm);
+        const float d0 = c * below(a.m, m), d1 = c * below(qm, m), f0 = __builtin_amdgcn_exp2f(d0), f1 = __builtin_amdgcn_exp2f(d1);
+        const float s0 = a.s == 0.f ? 0.f : f0 * a.s, t0 = a.s == 0.f ? 0.f : f0 * (a.t + fmaxf(d0, NO_SHARE) * a.s);
+        const float s1 = q.s == 0.f ? 0.f : f1 * q.s, t1 = q.s == 0.f ? 0.f : f1 * (q.t + fmaxf(d1, NO_SHARE) * q.s);
+        a = {m, s0 + s1, t0 + t1};
+    }
+    return block_stat(a, c, sh, [] {});
+}
+
+template <int TYPE, bool TOP>
+__global__ __launch_bounds__(THREADS) void logprobs_join_kernel(const LogprobsParams p) {
+    using Val = typename Kind<TYPE>::Val;
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    const uint32_t tid = threadIdx.x, row = blockIdx.x;
+    const Part *parts = p.parts + (size_t)row * p.chunks;
+    const Stat<Val> all = join_parts<Val>(parts, p.chunks, p.l.scale * LOG2E, sh);
+    if constexpr (TOP) {
+        const uint2 *lists = p.lists + (size_t)row * p.chunks * p.list_cap;
+        auto each = [&](auto f) {   // a wave a list
+            for (uint32_t q = tid >> 6; q < p.chunks; q += THREADS / 64) {
+                const uint32_t n = parts[q].listed;
+                for (uint32_t i = tid & 63; i < n; i += 64) {
+                    const uint2 w = lists[(size_t)q * p.list_cap + i];
+                    f(w.x, ~w.y);
+                }
+            }
+        };
+        uint32_t best = 0;
+        each([&](uint32_t key, uint32_t) { best = max(best, key); });
+        sh.key[tid] = best;
+        if (tid == 0) sh.listed = 0;
+        __syncthreads();
+        const uint32_t bound = key_bound<LOW_BITS<Val>>(sh, p.top);
+        each([&](uint32_t key, uint32_t cls) {
+            if (key >= bound) {
+                const uint32_t at = atomicAdd(&sh.listed, 1u);
+                if (at < LIST) sh.list[at] = make_uint2(key, ~cls);
+            }
+        });
+        __syncthreads();
+        if (sh.listed > LIST) {
+            __syncthreads();
+            list_exactly(each, p.top, sh);
+        }
+    }
+    finish_logprobs<TYPE>(p, p.row0 + row, all, sh);
+}
+
+template <class Val>
+struct OldStat {
+    Val m;
+    float s, t;
     __device__ __forceinline__ void clear() { m = lowest(m); s = 0.f; t = 0.f; }
-    __device__ __forceinline__ void join(const Stat &o, float scale) {
+    __device__ __forceinline__ void join(const OldStat &o, float scale) {
         const Val top = larger(m, o.m);
         const float d0 = scale * below(m, top), d1 = scale * below(o.m, top);
         const float f0 = s == 0.f ? 0.f : expf(d0), f1 = o.s == 0.f ? 0.f : expf(d1);
@@ -67,13 +429,12 @@ struct Stat {
     }
 };
 
-constexpr int THREADS = 256;
 
 template <class Val>
-__device__ Stat<Val> block_join(Stat<Val> a, float scale, Stat<Val> *part) {
+__device__ OldStat<Val> block_join(OldStat<Val> a, float scale, OldStat<Val> *part) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) {
-        Stat<Val> o;
+        OldStat<Val> o;
         o.m = __shfl_xor(a.m, off, 64); o.s = __shfl_xor(a.s, off, 64); o.t = __shfl_xor(a.t, off, 64);
         a.join(o, scale);
     }
@@ -87,76 +448,19 @@ __device__ Stat<Val> block_join(Stat<Val> a, float scale, Stat<Val> *part) {
 
 // Statistics of one row by a workgroup; `skip(j)`: classes that are left out.
 template <int TYPE, class Skip>
-__device__ Stat<typename Kind<TYPE>::Val> row_stat(const typename Kind<TYPE>::Raw *x, uint32_t classes, float scale, Stat<typename Kind<TYPE>::Val> *part, Skip skip) {
-    Stat<typename Kind<TYPE>::Val> a;
+__device__ OldStat<typename Kind<TYPE>::Val> row_stat(const typename Kind<TYPE>::Raw *x, uint32_t classes, float scale, OldStat<typename Kind<TYPE>::Val> *part, Skip skip) {
+    OldStat<typename Kind<TYPE>::Val> a;
     a.clear();
     for (uint32_t j = threadIdx.x; j < classes; j += THREADS) {
         if (skip(j)) continue;
         const auto v = Kind<TYPE>::val(x[j]);
-        Stat<typename Kind<TYPE>::Val> one;
+        OldStat<typename Kind<TYPE>::Val> one;
         one.m = v; one.s = possible(v) ? 1.f : 0.f; one.t = 0.f;
         if (one.s == 0.f && v != v) one.s = v;
         if ((float)v == -NEG_INF) one.s = __builtin_nanf("");
         a.join(one, scale);
     }
     return block_join(a, scale, part);
-}
-
-template <int TYPE>
-__global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams p) {
-    using K = Kind<TYPE>;
-    using Val = typename K::Val;
-    __shared__ Stat<Val> part[THREADS / 64];
-    __shared__ Val best_v[THREADS / 64];
-    __shared__ int best_i[THREADS / 64];
-    for (uint64_t r = blockIdx.x; r < p.l.rows; r += gridDim.x) {
-        const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
-        const Stat<Val> a = row_stat<TYPE>(x, p.l.classes, p.l.scale, part, [](uint32_t) { return false; });
-        const bool bad = a.s != a.s, empty = a.s == 0.f;
-        const float logs = empty ? 0.f : logf(a.s), nan = __builtin_nanf("");
-        if (threadIdx.x == 0) {
-            if (p.entropy) p.entropy[r] = bad ? nan : empty ? 0.f : logs - a.t / a.s;
-            if (p.stats) { p.stats[2 * r] = bits_of(a.m); p.stats[2 * r + 1] = bad ? nan : empty ? NEG_INF : logs; }
-        }
-        for (uint32_t g = threadIdx.x; g < p.n_given; g += THREADS) {
-            const int32_t c = p.given[r * p.n_given + g];
-            float lp = nan;
-            if (c < 0) lp = 0.f;
-            else if ((uint32_t)c < p.l.classes && !bad) {
-                const Val v = K::val(x[c]);
-                lp = possible(v) ? p.l.scale * below(v, a.m) - logs : NEG_INF;
-            }
-            p.logprob[r * p.n_given + g] = lp;
-        }
-        // the largest of those behind the last one taken
-        Val last_v = lowest(Val());
-        int last_i = -1;
-        for (uint32_t k = 0; k < p.top; ++k) {
-            Val bv = lowest(Val());
-            int bi = INT32_MAX;
-            if (!bad)
-                for (uint32_t j = threadIdx.x; j < p.l.classes; j += THREADS) {
-                    const Val v = K::val(x[j]);
-                    const bool open = possible(v) && (k == 0 || v < last_v || (v == last_v && (int)j > last_i));
-                    if (open && (bi == INT32_MAX || v > bv)) { bv = v; bi = (int)j; }
-                }
-            auto take = [&](Val ov, int oi) { if (oi != INT32_MAX && (bi == INT32_MAX || ov > bv || (ov == bv && oi < bi))) { bv = ov; bi = oi; } };
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) take(__shfl_xor(bv, off, 64), __shfl_xor(bi, off, 64));
-            if ((threadIdx.x & 63) == 0) { best_v[threadIdx.x >> 6] = bv; best_i[threadIdx.x >> 6] = bi; }
-            __syncthreads();
-            for (int w = 0; w < THREADS / 64; ++w) take(best_v[w], best_i[w]);
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                const bool none = bi == INT32_MAX;
-                p.top_class[r * p.top + k] = none ? -1 : bi;
-                p.top_logprob[r * p.top + k] = bad ? nan : none ? NEG_INF : p.l.scale * below(bv, a.m) - logs;
-            }
-            if (bi == INT32_MAX) bi = INT32_MAX - 1;   // nothing is behind it
-            last_v = bv;
-            last_i = bi;
-        }
-    }
 }
 
 template <int TYPE>
@@ -211,7 +515,7 @@ template <int TYPE>
 __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
-    __shared__ Stat<Val> part[THREADS / 64];
+    __shared__ OldStat<Val> part[THREADS / 64];
     __shared__ int entry[ISR_MAX_GIVEN];
     const float nan = __builtin_nanf("");
     for (uint64_t r = blockIdx.x; r < p.l.rows; r += gridDim.x) {
@@ -237,8 +541,8 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p)
             }
             continue;
         }
-        const Stat<Val> a = row_stat<TYPE>(x, p.l.classes, p.l.scale, part, [](uint32_t) { return false; });
-        Stat<Val> b = a;
+        const OldStat<Val> a = row_stat<TYPE>(x, p.l.classes, p.l.scale, part, [](uint32_t) { return false; });
+        OldStat<Val> b = a;
         if (p.rest) b = row_stat<TYPE>(x, p.l.classes, p.l.scale, part, [&](uint32_t j) {
             for (uint32_t i = 0; i < p.top; ++i)
                 if (entry[i] == (int)j) return true;
@@ -325,7 +629,61 @@ static unsigned row_grid(uint64_t rows) { return (unsigned)(rows < (1u << 20) ? 
     }                                                                                                                        \
     return hipGetLastError()
 
-hipError_t launch_logprobs(const LogprobsParams &p, hipStream_t st) { LAUNCH_BY_TYPE(logprobs_kernel, p, st); }
+
+// ---- launches ------------------------------------------------------------------------
+
+template <int TYPE, int NV>
+static void launch_chunks(const LogprobsParams &p, uint32_t rows, hipStream_t st) {
+    const dim3 grid(rows * p.chunks), block(THREADS);
+    if (p.top && p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, true, true>), grid, block, 0, st, p);
+    else if (p.top) hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, true, false>), grid, block, 0, st, p);
+    else if (p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, false, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, false, false>), grid, block, 0, st, p);
+}
+
+template <int TYPE>
+static void launch_rows(const LogprobsParams &p, uint32_t nv, uint32_t rows, hipStream_t st) {
+    if (nv == 2) launch_chunks<TYPE, 2>(p, rows, st);
+    else launch_chunks<TYPE, 8>(p, rows, st);
+    if (p.chunks == 1) return;
+    if (p.top) hipLaunchKernelGGL((logprobs_join_kernel<TYPE, true>), dim3(rows), dim3(THREADS), 0, st, p);
+    else hipLaunchKernelGGL((logprobs_join_kernel<TYPE, false>), dim3(rows), dim3(THREADS), 0, st, p);
+}
+
+RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top) {
+    RowCut cut;
+    const uint32_t per_vec = type == ISR_F32 || type == ISR_I32 ? 4 : 8, vecs = classes / per_vec;
+    auto chunks_of = [&](uint32_t nv) { return vecs <= nv * THREADS ? 1 : (vecs + nv * THREADS - 1) / (nv * THREADS); };
+    cut.nv = rows * chunks_of(8) >= 1024 ? 8 : 2;
+    cut.chunks = chunks_of(cut.nv);
+    cut.chunk_vecs = vecs ? (vecs + cut.chunks - 1) / cut.chunks : 1;
+    cut.list_cap = cut.chunks == 1 ? LIST : 2 * top + 64;
+    const uint64_t most = (1u << 22) / cut.chunks;   // workgroups of a launch
+    cut.rows = (uint32_t)std::min<uint64_t>(rows, most ? most : 1);
+    cut.parts_bytes = cut.chunks == 1 ? 0 : ((size_t)cut.rows * cut.chunks * sizeof(Part) + 255) / 256 * 256;
+    cut.lists_bytes = cut.chunks == 1 || !top ? 0 : (size_t)cut.rows * cut.chunks * cut.list_cap * sizeof(uint2);
+    return cut;
+}
+
+hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st) {
+    p.chunks = cut.chunks;
+    p.chunk_vecs = cut.chunk_vecs;
+    p.list_cap = cut.list_cap;
+    p.parts = (Part *)workspace;
+    p.lists = (uint2 *)((uint8_t *)workspace + cut.parts_bytes);
+    for (p.row0 = 0; p.row0 < p.l.rows; p.row0 += cut.rows) {
+        const uint32_t rows = (uint32_t)std::min<uint64_t>(cut.rows, p.l.rows - p.row0);
+        switch (p.l.type) {
+        case ISR_F32: launch_rows<ISR_F32>(p, cut.nv, rows, st); break;
+        case ISR_BF16: launch_rows<ISR_BF16>(p, cut.nv, rows, st); break;
+        case ISR_F16: launch_rows<ISR_F16>(p, cut.nv, rows, st); break;
+        default: launch_rows<ISR_I32>(p, cut.nv, rows, st); break;
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 hipError_t launch_logprobs_grad(const LogprobsGradParams &p, hipStream_t st) { LAUNCH_BY_TYPE(logprobs_grad_kernel, p, st); }
 hipError_t launch_distill(const DistillParams &p, hipStream_t st) { LAUNCH_BY_TYPE(distill_kernel, p, st); }
 hipError_t launch_distill_grad(const DistillParams &p, hipStream_t st) { LAUNCH_BY_TYPE(distill_grad_kernel, p, st); }
