@@ -61,7 +61,11 @@ LogitRows rows_of(const isr_logits *l) { return {l->data_device, l->type, l->cla
 
 DistillParams distill_params(const isr_logits *l, const isr_teacher *t, const float *weight, float *loss, float *stats, void *grad,
                              uint64_t grad_stride) {
-    return {rows_of(l), t->class_device, t->logit_device, t->type, t->top, t->scale, t->rest, weight, loss, stats, grad, grad_stride};
+    DistillParams p{};
+    p.l = rows_of(l);
+    p.entry = t->class_device; p.value = t->logit_device; p.value_type = t->type; p.top = t->top; p.value_scale = t->scale; p.rest = t->rest;
+    p.weight = weight; p.loss = loss; p.stats = stats; p.grad = grad; p.grad_stride = grad_stride;
+    return p;
 }
 
 int status(hipError_t e) {
@@ -110,14 +114,18 @@ int isr_logprobs_grad(const isr_logits *l, const int32_t *given_device, uint32_t
     if (given && (!given_device || !grad_logprob_device)) return ISR_ERR_ARG;
     if (!stats_device || !all_aligned({given_device, grad_logprob_device, entropy_device, grad_entropy_device, stats_device})) return ISR_ERR_ARG;
     if (!valid_grad(l, grad_logits_device, grad_row_stride)) return ISR_ERR_ARG;
-    return status(launch_logprobs_grad({rows_of(l), given_device, given, grad_logprob_device, entropy_device, grad_entropy_device, stats_device,
-                                        grad_logits_device, grad_row_stride}, (hipStream_t)hip_stream));
+    LogprobsGradParams p{};
+    p.l = rows_of(l);
+    p.given = given_device; p.n_given = given;
+    p.up_logprob = grad_logprob_device; p.entropy = entropy_device; p.up_entropy = grad_entropy_device; p.stats = stats_device;
+    p.grad = grad_logits_device; p.grad_stride = grad_row_stride;
+    return status(launch_logprobs_grad(p, (hipStream_t)hip_stream));
 }
 
-// one row's statistics when the caller keeps none: the gradient's kernel reads them
+// what the chunks of rows leave, and the rows' statistics when the caller keeps none: the gradient's kernel reads them
 size_t isr_distill_workspace_bytes(const isr_logits *l, const isr_teacher *t) {
-    if (!valid_shape(l) || !valid_teacher(t)) return 0;
-    return l->rows * DISTILL_STATS;
+    if (!valid_shape(l) || !valid_teacher(t) || l->rows == 0) return 0;
+    return cut_rows(l->type, l->classes, l->rows, 0).parts_bytes + l->rows * DISTILL_STATS;
 }
 
 int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weight_device, float *loss_device, float *stats_device,
@@ -128,8 +136,10 @@ int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weig
     if (grad_logits_device && !valid_grad(l, grad_logits_device, grad_row_stride)) return ISR_ERR_ARG;
     if (!workspace_device || workspace_bytes < isr_distill_workspace_bytes(l, t)) return ISR_ERR_WORKSPACE;
     if (!aligned(workspace_device, 16)) return ISR_ERR_ARG;
-    DistillParams p = distill_params(l, t, row_weight_device, loss_device, stats_device ? stats_device : (float *)workspace_device, grad_logits_device, grad_row_stride);
-    hipError_t e = launch_distill(p, (hipStream_t)hip_stream);
+    const RowCut cut = cut_rows(l->type, l->classes, l->rows, 0);
+    float *stats = stats_device || !grad_logits_device ? stats_device : (float *)((uint8_t *)workspace_device + cut.parts_bytes);
+    const DistillParams p = distill_params(l, t, row_weight_device, loss_device, stats, grad_logits_device, grad_row_stride);
+    hipError_t e = launch_distill(p, cut, workspace_device, (hipStream_t)hip_stream);
     if (e == hipSuccess && grad_logits_device) e = launch_distill_grad(p, (hipStream_t)hip_stream);
     return status(e);
 }

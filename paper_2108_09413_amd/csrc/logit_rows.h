@@ -45,6 +45,9 @@ struct LogprobsGradParams {
     const float *up_logprob, *entropy, *up_entropy, *stats;
     void *grad;
     uint64_t grad_stride;
+    // set by the launcher
+    uint64_t row0;
+    uint32_t chunks, chunk_vecs;
 };
 
 struct DistillParams {
@@ -59,11 +62,15 @@ struct DistillParams {
     float *loss, *stats;      // stats: [rows][8], DistillStat
     void *grad;
     uint64_t grad_stride;
+    // set by the launcher
+    uint64_t row0;
+    uint32_t chunks, chunk_vecs;
+    Part *parts;
 };
 
 hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st);
-hipError_t launch_logprobs_grad(const LogprobsGradParams &p, hipStream_t st);
-hipError_t launch_distill(const DistillParams &p, hipStream_t st);
-hipError_t launch_distill_grad(const DistillParams &p, hipStream_t st);
+hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st);
+hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st);
+hipError_t launch_distill_grad(DistillParams p, hipStream_t st);
 
 }  // namespace isr

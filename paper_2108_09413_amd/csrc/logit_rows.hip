@@ -92,18 +92,20 @@ struct Stat {
     float s, t;
 };
 
-struct Shared {
-    uint32_t key[THREADS];      // largest key of each thread
-    uint2 list[LIST + 2];       // candidates: (key, ~class), so that the larger 64-bit number comes first
+struct SharedStat {
     uint32_t m[THREADS / 64];   // Val
     float s[THREADS / 64], t[THREADS / 64];
-    int count[THREADS / 64];
+};
+struct Shared : SharedStat {
     uint32_t listed;
+    int count[THREADS / 64];
+    alignas(16) uint32_t key[THREADS];   // largest key of each thread
+    alignas(16) uint2 list[LIST + 2];    // candidates: (key, ~class), so that the larger 64-bit number comes first
 };
 
 // The workgroup's statistics from those of its threads.  Two barriers; `with_keys` has something stored before the first.
 template <class Val, class Between>
-__device__ __forceinline__ Stat<Val> block_stat(Stat<Val> a, float c, Shared &sh, Between with_keys) {
+__device__ __forceinline__ Stat<Val> block_stat(Stat<Val> a, float c, SharedStat &sh, Between with_keys) {
     const int wave = threadIdx.x >> 6;
     const Val wm = wave_max(a.m);
     if ((threadIdx.x & 63) == 0) sh.m[wave] = __builtin_bit_cast(uint32_t, wm);
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
 
 // The chunks of a row together.
 template <class Val>
-__device__ __forceinline__ Stat<Val> join_parts(const Part *parts, uint32_t chunks, float c, Shared &sh) {
+__device__ __forceinline__ Stat<Val> join_parts(const Part *parts, uint32_t chunks, float c, SharedStat &sh) {
     Stat<Val> a{lowest(Val()), 0.f, 0.f};
     for (uint32_t i = threadIdx.x; i < chunks; i += THREADS) {
         const Part q = parts[i];
@@ -414,221 +416,381 @@ __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(const LogprobsPa
     finish_logprobs<TYPE>(p, p.row0 + row, all, sh);
 }
 
-template <class Val>
-struct OldStat {
-    Val m;
-    float s, t;
-    __device__ __forceinline__ void clear() { m = lowest(m); s = 0.f; t = 0.f; }
-    __device__ __forceinline__ void join(const OldStat &o, float scale) {
-        const Val top = larger(m, o.m);
-        const float d0 = scale * below(m, top), d1 = scale * below(o.m, top);
-        const float f0 = s == 0.f ? 0.f : expf(d0), f1 = o.s == 0.f ? 0.f : expf(d1);
-        t = f0 * (t + (f0 == 0.f ? 0.f : d0 * s)) + f1 * (o.t + (f1 == 0.f ? 0.f : d1 * o.s));
-        s = f0 * s + f1 * o.s;
-        m = top;
-    }
-};
+// ---- distillation -----------------------------------------------------------------------
 
-
-template <class Val>
-__device__ OldStat<Val> block_join(OldStat<Val> a, float scale, OldStat<Val> *part) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        OldStat<Val> o;
-        o.m = __shfl_xor(a.m, off, 64); o.s = __shfl_xor(a.s, off, 64); o.t = __shfl_xor(a.t, off, 64);
-        a.join(o, scale);
-    }
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
-    __syncthreads();
-    a = part[0];
-    for (int w = 1; w < THREADS / 64; ++w) a.join(part[w], scale);
-    __syncthreads();
-    return a;
-}
-
-// Statistics of one row by a workgroup; `skip(j)`: classes that are left out.
-template <int TYPE, class Skip>
-__device__ OldStat<typename Kind<TYPE>::Val> row_stat(const typename Kind<TYPE>::Raw *x, uint32_t classes, float scale, OldStat<typename Kind<TYPE>::Val> *part, Skip skip) {
-    OldStat<typename Kind<TYPE>::Val> a;
-    a.clear();
-    for (uint32_t j = threadIdx.x; j < classes; j += THREADS) {
-        if (skip(j)) continue;
-        const auto v = Kind<TYPE>::val(x[j]);
-        OldStat<typename Kind<TYPE>::Val> one;
-        one.m = v; one.s = possible(v) ? 1.f : 0.f; one.t = 0.f;
-        if (one.s == 0.f && v != v) one.s = v;
-        if ((float)v == -NEG_INF) one.s = __builtin_nanf("");
-        a.join(one, scale);
-    }
-    return block_join(a, scale, part);
-}
-
-template <int TYPE>
-__global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(const LogprobsGradParams p) {
-    using K = Kind<TYPE>;
-    using Val = typename K::Val;
-    for (uint64_t r = blockIdx.x; r < p.l.rows; r += gridDim.x) {
-        const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
-        auto *out = (typename K::Grad *)p.grad + r * p.grad_stride;
-        const Val m = of_bits<Val>(p.stats[2 * r]);
-        const float logs = p.stats[2 * r + 1], uh = p.up_entropy ? p.up_entropy[r] : 0.f, h = uh != 0.f ? p.entropy[r] : 0.f;
-        float up = 0.f;
-        bool any = uh != 0.f;
-        for (uint32_t g = 0; g < p.n_given; ++g) {
-            const int32_t c = p.given[r * p.n_given + g];
-            if (c < 0) continue;
-            any = true;
-            up += (uint32_t)c < p.l.classes ? p.up_logprob[r * p.n_given + g] : __builtin_nanf("");
-        }
-        const bool zero = !any || logs == NEG_INF;
-        for (uint32_t j = threadIdx.x; j < p.l.classes; j += THREADS) {
-            float g = 0.f;
-            if (!zero) {
-                const float lp = p.l.scale * below(K::val(x[j]), m) - logs, pr = expf(lp);
-                g = -pr * up;
-                if (uh != 0.f && pr != 0.f) g -= uh * pr * (lp + h);
-                for (uint32_t i = 0; i < p.n_given; ++i)
-                    if (p.given[r * p.n_given + i] == (int32_t)j) g += p.up_logprob[r * p.n_given + i];
-                g *= p.l.scale;
-            }
-            out[j] = K::grad(g);
-        }
-    }
-}
-
-// Statistics of a row between the loss and its gradient.  zero: neither an entry nor a possible class, the gradient is zero.
+// Statistics of a row between the loss and its gradient.  logs == -infinity: the gradient is zero.
 struct DistillStat {
-    float m, logs;           // of all classes
-    float rest_m, rest_logs; // of those that are no entry (rest)
+    float m, logs;               // of all classes; m: Val
+    float rest_m, rest_logs;     // of those that are no entry (rest), else as m and logs
     float value_m, value_logs;   // q = exp(value_scale (value - value_m) - value_logs)
-    float total, left;       // sum of q (and q_rest); q_rest
+    float total, left;           // sum of q and q_rest; q_rest
 };
 static_assert(sizeof(DistillStat) == 32, "eight words a row");
 
 __device__ __forceinline__ float teacher_value(const void *p, int type, uint64_t i) {
     if (type == ISR_F32) return ((const float *)p)[i];
     if (type == ISR_BF16) return Kind<ISR_BF16>::val(((const uint16_t *)p)[i]);
-    return (float)((const _Float16 *)p)[i];
+    return Kind<ISR_F16>::val(((const _Float16 *)p)[i]);
 }
 
+// Up to 128 named classes of a row, two a lane: of index lane and lane + 64.
+struct Named {
+    int32_t c[2];   // negative: none
+    __device__ __forceinline__ void load(const int32_t *p, uint32_t n) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t i = (threadIdx.x & 63) + 64 * h;
+            c[h] = i < n ? p[i] : -1;
+        }
+    }
+    // visit(h, j, same): for each of the lane's two and each j < n in ascending order, whether they name one class
+    template <class Visit>
+    __device__ __forceinline__ void pairs(uint32_t n, Visit visit) const {
+        for (uint32_t j = 0; j < n; ++j) {
+            const int other = j < 64 ? __builtin_amdgcn_readlane(c[0], j) : __builtin_amdgcn_readlane(c[1], j - 64);
+            visit(0, j, other == c[0]);
+            if (n > 64) visit(1, j, other == c[1]);
+        }
+    }
+    // whether the class is the first of its name
+    __device__ __forceinline__ void first(uint32_t n, bool (&is)[2]) const {
+        const uint32_t lane = threadIdx.x & 63;
+        is[0] = c[0] >= 0;
+        is[1] = c[1] >= 0;
+        pairs(n, [&](int h, uint32_t j, bool same) { if (same && j < lane + 64 * h) is[h] = false; });
+    }
+};
+
+// Loss and statistics of a row, by one wave, from the statistics of all classes or (rest) of those that are no entry.  A few
+// hundred operations a row, in 64 bits: q_rest is next to 0 where the entries hold nearly all, and the loss of a student close
+// to its teacher is a sum that cancels.
 template <int TYPE>
+__device__ void finish_distill(const DistillParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a) {
+    using K = Kind<TYPE>;
+    using Val = typename K::Val;
+    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+    const uint32_t lane = threadIdx.x & 63;
+    Named e;
+    e.load(p.entry + r * p.top, p.top);
+    float v[2];
+    bool bad = false;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        v[h] = e.c[h] >= 0 ? teacher_value(p.value, p.value_type, r * p.top + lane + 64 * h) : NEG_INF;
+        bad |= e.c[h] >= 0 && ((uint32_t)e.c[h] >= p.l.classes || v[h] != v[h] || v[h] == -NEG_INF);
+    }
+    const bool any = __any(e.c[0] >= 0 || e.c[1] >= 0);
+    bad = __any(bad);
+    const float vm = p.rest ? 0.f : wave_max(larger(v[0], v[1]));
+    if (!any || vm == NEG_INF) {
+        if (lane == 0) {
+            p.loss[r] = 0.f;
+            if (p.stats) *(DistillStat *)(p.stats + 8 * r) = DistillStat{0.f, NEG_INF, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        }
+        return;
+    }
+    const float c = p.l.scale * LOG2E;
+    double lq[2], q[2];
+    Val at[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        lq[h] = (double)p.value_scale * ((double)v[h] - vm);
+        q[h] = exp(lq[h]);
+        at[h] = e.c[h] >= 0 && (uint32_t)e.c[h] < p.l.classes ? K::val(x[e.c[h]]) : lowest(Val());
+    }
+    double total = wave_sum(q[0] + q[1]), value_logs = 0.0, left = 0.0;
+    Stat<Val> all = a;
+    if (p.rest) {
+        left = fmax(1.0 - total, 0.0);
+        bool is[2];
+        e.first(p.top, is);
+        all.m = larger(a.m, wave_max(larger(is[0] ? at[0] : lowest(Val()), is[1] ? at[1] : lowest(Val()))));
+        float s = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (is[h]) s += __builtin_amdgcn_exp2f(c * below(at[h], all.m));
+        all.s = wave_sum(s) + (a.s == 0.f ? 0.f : a.s * __builtin_amdgcn_exp2f(c * below(a.m, all.m)));
+    } else {
+        value_logs = log(total);
+        total = 0.0;
+    }
+    const bool empty = all.s == 0.f;
+    const double logs = empty ? 0.0 : log((double)all.s), rest_logs = a.s == 0.f ? (double)NEG_INF : log((double)a.s);
+    double loss = 0.0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (!p.rest) { lq[h] -= value_logs; q[h] = exp(lq[h]); total += q[h]; }
+        const double lp = empty || !possible(at[h]) ? (double)NEG_INF : (double)p.l.scale * below64(at[h], all.m) - logs;
+        if (e.c[h] >= 0 && q[h] > 0.0) loss += q[h] * (lq[h] - lp);
+    }
+    loss = wave_sum(loss);
+    if (!p.rest) total = wave_sum(total);
+    if (left > 0.0) {
+        const double lr = a.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(a.m, all.m) + rest_logs - logs;
+        loss += left * (log(left) - lr);
+    }
+    total += left;
+    if (bad || all.s != all.s) loss = total = __builtin_nan("");
+    if (lane != 0) return;
+    p.loss[r] = (float)loss;
+    if (p.stats)
+        *(DistillStat *)(p.stats + 8 * r) = DistillStat{bits_of(all.m), empty ? NEG_INF : (float)logs, bits_of(a.m), (float)rest_logs,
+                                                         vm, (float)value_logs, (float)total, (float)left};
+}
+
+// The chunk of a row as in logprobs_kernel.  REST: without the entries, which a byte of bits for each vector in LDS tells: a
+// thread's NV bytes are one read, and vectors without an entry (nearly all) go the same way as in the other case.
+template <int TYPE, int NV, bool REST>
 __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
-    __shared__ OldStat<Val> part[THREADS / 64];
-    __shared__ int entry[ISR_MAX_GIVEN];
-    const float nan = __builtin_nanf("");
-    for (uint64_t r = blockIdx.x; r < p.l.rows; r += gridDim.x) {
-        const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
-        __syncthreads();
-        if (threadIdx.x < p.top) entry[threadIdx.x] = p.entry[r * p.top + threadIdx.x];
-        __syncthreads();
-        bool any = false, outside = false;
-        float vm = NEG_INF;
-        for (uint32_t i = 0; i < p.top; ++i) {
-            if (entry[i] < 0) continue;
-            any = true;
-            outside |= (uint32_t)entry[i] >= p.l.classes;
-            const float v = teacher_value(p.value, p.value_type, r * p.top + i);
-            if (v != v || v == -NEG_INF) outside = true;
-            vm = fmaxf(vm, v);
-        }
-        if (p.rest) vm = 0.f;
-        if (!any || vm == NEG_INF) {
-            if (threadIdx.x == 0) {
-                p.loss[r] = 0.f;
-                if (p.stats) *(DistillStat *)(p.stats + 8 * r) = DistillStat{0.f, NEG_INF, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            }
-            continue;
-        }
-        const OldStat<Val> a = row_stat<TYPE>(x, p.l.classes, p.l.scale, part, [](uint32_t) { return false; });
-        OldStat<Val> b = a;
-        if (p.rest) b = row_stat<TYPE>(x, p.l.classes, p.l.scale, part, [&](uint32_t j) {
-            for (uint32_t i = 0; i < p.top; ++i)
-                if (entry[i] == (int)j) return true;
-            return false;
-        });
-        if (threadIdx.x != 0) continue;
-        const bool empty = a.s == 0.f;
-        const double logs = empty ? 0.0 : log((double)a.s), rest_logs = b.s == 0.f ? NEG_INF : log((double)b.s);
-        double z = 0.0;
-        for (uint32_t i = 0; i < p.top; ++i)
-            if (entry[i] >= 0) z += exp((double)p.value_scale * ((double)teacher_value(p.value, p.value_type, r * p.top + i) - vm));
-        const double value_logs = p.rest ? 0.0 : log(z);
-        double loss = 0.0, total = 0.0;
-        for (uint32_t i = 0; i < p.top; ++i) {
-            if (entry[i] < 0 || (uint32_t)entry[i] >= p.l.classes) continue;
-            const double logq = (double)p.value_scale * ((double)teacher_value(p.value, p.value_type, r * p.top + i) - vm) - value_logs, q = exp(logq);
-            total += q;
-            const Val v = K::val(x[entry[i]]);
-            const double logp = empty || !possible(v) ? (double)NEG_INF : (double)p.l.scale * below64(v, a.m) - logs;
-            if (q > 0.0) loss += q * (logq - logp);
-        }
-        double left = 0.0;
-        if (p.rest) {
-            left = 1.0 - total > 0.0 ? 1.0 - total : 0.0;
-            total += left;
-            const double logr = b.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(b.m, a.m) + rest_logs - logs;
-            if (left > 0.0) loss += left * (log(left) - logr);
-        }
-        if (outside || a.s != a.s) loss = total = nan;
-        p.loss[r] = (float)loss;
-        if (p.stats)
-            *(DistillStat *)(p.stats + 8 * r) = DistillStat{bits_of(a.m), empty ? NEG_INF : (float)logs, bits_of(b.m), (float)rest_logs,
-                                                             vm, (float)value_logs, (float)total, (float)left};
+    constexpr int PV = PER_VEC<TYPE>;
+    __shared__ SharedStat sh;
+    __shared__ __attribute__((aligned(8))) uint32_t mask[REST ? NV * THREADS / 4 : 1];
+    __shared__ uint32_t tail_mask;
+    const uint32_t tid = threadIdx.x, row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks;
+    const uint64_t r = p.row0 + row;
+    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+    const uint32_t vecs = p.l.classes / PV, v0 = chunk * p.chunk_vecs, n = min(p.chunk_vecs, vecs - min(vecs, v0));
+    const uint32_t rest = vecs * PV + tid;
+    bool tail = chunk == p.chunks - 1 && rest < p.l.classes;
+    uint4 raw[NV];
+    if (n) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = ((const Loose *)(x + (size_t)(v0 + min(i * THREADS + tid, n - 1)) * PV))->v;
     }
+    const Val edge = tail ? K::val(x[rest]) : lowest(Val());
+    uint32_t out[NV / 4 ? NV / 4 : 1] = {};   // bits of the entries among this thread's vectors, a byte each
+    if constexpr (REST) {
+        for (int i = tid; i < NV * THREADS / 4; i += THREADS) mask[i] = 0;
+        if (tid == 0) tail_mask = 0;
+        const int32_t e = tid < p.top ? p.entry[r * p.top + tid] : -1;
+        __syncthreads();
+        const uint32_t j = (uint32_t)e - v0 * PV;
+        if (e >= 0 && (uint32_t)e >= v0 * PV && j < n * PV) {
+            const uint32_t vec = j / PV, byte = vec % THREADS * NV + vec / THREADS;
+            atomicOr(&mask[byte >> 2], 1u << (8 * (byte & 3) + j % PV));
+        } else if (e >= 0 && (uint32_t)e >= vecs * PV && (uint32_t)e < p.l.classes) {
+            atomicOr(&tail_mask, 1u << ((uint32_t)e - vecs * PV));
+        }
+        __syncthreads();
+        if constexpr (NV == 8) {
+            const uint2 w = *(const uint2 *)&mask[tid * 2];
+            out[0] = w.x;
+            out[1] = w.y;
+        } else {
+            static_assert(NV == 2);
+            out[0] = ((const uint16_t *)mask)[tid];
+        }
+        tail = tail && !(tail_mask >> tid & 1);
+    }
+    auto bits = [&](int i) { return out[i / 4] >> (8 * (i & 3)) & 0xFF; };
+    Stat<Val> a{tail ? edge : lowest(Val()), 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * THREADS + tid >= n) continue;
+        Val v[PV];
+        unpack<TYPE>(raw[i], v);
+        if (REST && bits(i)) {
+#pragma unroll
+            for (int e = 0; e < PV; ++e) v[e] = bits(i) >> e & 1 ? lowest(Val()) : v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < PV; ++e) a.m = larger(a.m, v[e]);
+    }
+    const float c = p.l.scale * LOG2E;
+    auto share = [&](Val v) { return __builtin_amdgcn_exp2f(c * below(v, a.m)); };
+    if (tail) a.s = share(edge);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * THREADS + tid >= n) continue;
+        Val v[PV];
+        unpack<TYPE>(raw[i], v);
+        if (REST && bits(i)) {
+#pragma unroll
+            for (int e = 0; e < PV; ++e) a.s += bits(i) >> e & 1 ? 0.f : share(v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < PV; ++e) a.s += share(v[e]);
+        }
+    }
+    const Stat<Val> all = block_stat(a, c, sh, [] {});
+    if (p.chunks == 1) {
+        if (tid < 64) finish_distill<TYPE>(p, r, all);
+        return;
+    }
+    if (tid == 0) p.parts[(size_t)row * p.chunks + chunk] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, 0.f, 0};
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillParams p) {
+__global__ __launch_bounds__(THREADS) void distill_join_kernel(const DistillParams p) {
+    using Val = typename Kind<TYPE>::Val;
+    __shared__ SharedStat sh;
+    const Stat<Val> all = join_parts<Val>(p.parts + (size_t)blockIdx.x * p.chunks, p.chunks, p.l.scale * LOG2E, sh);
+    if (threadIdx.x < 64) finish_distill<TYPE>(p, p.row0 + blockIdx.x, all);
+}
+
+// ---- gradients --------------------------------------------------------------------------
+
+// A chunk of a gradient's row: with d = c (x - m) - l2 the log2 of a probability, every element gets 2^d (a0 + a1 d), and the
+// named classes what `special(h, x)` says of them.  Their logits are read before anything is stored (the gradient may go
+// over the logits) and theirs is stored behind all others' (a barrier each, in chunks that hold one).
+template <class Val>
+struct Slope {
+    Val m;
+    float l2, a0, a1;
+    bool zero;   // the row's gradient is zero
+};
+
+template <int TYPE, int NV, bool LINEAR, class Params, class Special>
+__device__ __forceinline__ void store_gradient(const Params &p, uint64_t r, uint32_t chunk, const Slope<typename Kind<TYPE>::Val> &f, const Named &named,
+                                               const bool (&first)[2], const uint4 (&raw)[NV], Special special) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
-    __shared__ int entry[ISR_MAX_GIVEN];
-    __shared__ float q[ISR_MAX_GIVEN];
-    for (uint64_t r = blockIdx.x; r < p.l.rows; r += gridDim.x) {
-        const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
-        auto *out = (typename K::Grad *)p.grad + r * p.grad_stride;
-        const DistillStat st = *(const DistillStat *)(p.stats + 8 * r);
-        __syncthreads();
-        if (threadIdx.x < p.top) {
-            entry[threadIdx.x] = p.entry[r * p.top + threadIdx.x];
-            q[threadIdx.x] = expf(p.value_scale * (teacher_value(p.value, p.value_type, r * p.top + threadIdx.x) - st.value_m) - st.value_logs);
+    constexpr int PV = PER_VEC<TYPE>;
+    const uint32_t tid = threadIdx.x;
+    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+    auto *out = (typename K::Grad *)p.grad + r * p.grad_stride;
+    const uint32_t vecs = p.l.classes / PV, v0 = chunk * p.chunk_vecs, n = min(p.chunk_vecs, vecs - min(vecs, v0));
+    const uint32_t rest = vecs * PV + tid, lo = min(v0, vecs) * PV, hi = chunk == p.chunks - 1 ? p.l.classes : lo + n * PV;
+    const bool tail = chunk == p.chunks - 1 && rest < p.l.classes;
+    const float c = p.l.scale * LOG2E;
+    auto value = [&](Val v) {
+        const float d = c * below(v, f.m) - f.l2, e = __builtin_amdgcn_exp2f(d);
+        return LINEAR ? e * (f.a0 + f.a1 * fmaxf(d, NO_SHARE)) : e * f.a0;
+    };
+    bool here[2];
+    float own[2] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) here[h] = !f.zero && named.c[h] >= 0 && (uint32_t)named.c[h] >= lo && (uint32_t)named.c[h] < hi;
+    const bool some = __any(here[0] || here[1]);   // the same in every wave
+    const Val edge = tail && !f.zero ? K::val(x[rest]) : lowest(Val());
+    if (some) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            here[h] = here[h] && first[h] && tid < 64;
+            if (here[h]) own[h] = special(h, K::val(x[named.c[h]]), value);
         }
         __syncthreads();
-        const float w = p.weight ? p.weight[r] : 1.f, f = p.l.scale * w;
-        const bool zero = w == 0.f || st.logs == NEG_INF;
-        const Val m = of_bits<Val>(st.m), rest_m = of_bits<Val>(st.rest_m);
-        const float logr = p.l.scale * below(rest_m, m) + st.rest_logs - st.logs;
-        const float rest_c = p.rest ? st.total * expf(logr) - st.left : 0.f;
-        for (uint32_t j = threadIdx.x; j < p.l.classes; j += THREADS) {
-            float g = 0.f;
-            if (!zero) {
-                const Val v = K::val(x[j]);
-                float sum = 0.f;
-                bool is_entry = false;
-                for (uint32_t i = 0; i < p.top; ++i)
-                    if (entry[i] == (int)j) { is_entry = true; sum += q[i]; }
-                if (!p.rest || is_entry) g = st.total * expf(p.l.scale * below(v, m) - st.logs) - sum;
-                else g = rest_c * (possible(v) ? expf(p.l.scale * below(v, rest_m) - st.rest_logs) : 0.f);   // NaN in a row of NaN
-                g *= f;
-            }
-            out[j] = K::grad(g);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * THREADS + tid >= n) continue;
+        typedef typename K::Grad Vec __attribute__((ext_vector_type(PV)));
+        Vec g = 0;
+        if (!f.zero) {
+            Val v[PV];
+            unpack<TYPE>(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < PV; ++e) g[e] = K::grad(value(v[e]));
         }
+        ((Loose *)(out + (size_t)(v0 + i * THREADS + tid) * PV))->v = __builtin_bit_cast(uint4, g);
+    }
+    if (tail) out[rest] = K::grad(f.zero ? 0.f : value(edge));
+    if (some) {
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (here[h]) out[named.c[h]] = K::grad(own[h]);
     }
 }
 
-static unsigned row_grid(uint64_t rows) { return (unsigned)(rows < (1u << 20) ? rows : (1u << 20)); }
+template <int TYPE, int NV, class Params>
+__device__ __forceinline__ void load_chunk(const Params &p, uint64_t r, uint32_t chunk, uint4 (&raw)[NV]) {
+    constexpr int PV = PER_VEC<TYPE>;
+    const auto *x = (const typename Kind<TYPE>::Raw *)p.l.x + r * p.l.stride;
+    const uint32_t vecs = p.l.classes / PV, v0 = chunk * p.chunk_vecs, n = min(p.chunk_vecs, vecs - min(vecs, v0));
+    if (n) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = ((const Loose *)(x + (size_t)(v0 + min(i * THREADS + threadIdx.x, n - 1)) * PV))->v;
+    }
+}
 
-#define LAUNCH_BY_TYPE(kernel, p, st)                                                                                        \
-    const dim3 grid(row_grid((p).l.rows)), block(THREADS);                                                                   \
-    switch ((p).l.type) {                                                                                                    \
-    case ISR_F32: hipLaunchKernelGGL((kernel<ISR_F32>), grid, block, 0, st, p); break;                                       \
-    case ISR_BF16: hipLaunchKernelGGL((kernel<ISR_BF16>), grid, block, 0, st, p); break;                                     \
-    case ISR_F16: hipLaunchKernelGGL((kernel<ISR_F16>), grid, block, 0, st, p); break;                                       \
-    default: hipLaunchKernelGGL((kernel<ISR_I32>), grid, block, 0, st, p); break;                                            \
-    }                                                                                                                        \
-    return hipGetLastError()
+// scale (sum_g u_g ([j = c_g] - p_j) - u_H p_j (log p_j + H))
+template <int TYPE, int NV, bool ENT>
+__global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(const LogprobsGradParams p) {
+    using Val = typename Kind<TYPE>::Val;
+    const uint32_t row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks, lane = threadIdx.x & 63;
+    const uint64_t r = p.row0 + row;
+    uint4 raw[NV];
+    load_chunk<TYPE, NV>(p, r, chunk, raw);
+    Named named;
+    named.load(p.given + r * p.n_given, p.n_given);
+    float u[2];
+    bool first[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t c = (uint32_t)named.c[h];
+        u[h] = named.c[h] < 0 ? 0.f : c < p.l.classes ? p.up_logprob[r * p.n_given + lane + 64 * h] : __builtin_nanf("");
+    }
+    float up = u[0], sum[2] = {u[0], u[1]};
+    if (p.n_given == 1) {
+        up = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u[0]), 0));
+        first[0] = named.c[0] >= 0;
+        first[1] = false;
+    } else {
+        up = wave_sum(u[0] + u[1]);
+        sum[0] = sum[1] = 0.f;
+        first[0] = named.c[0] >= 0;
+        first[1] = named.c[1] >= 0;
+        named.pairs(p.n_given, [&](int h, uint32_t j, bool same) {
+            const float uj = __int_as_float(j < 64 ? __builtin_amdgcn_readlane(__float_as_int(u[0]), j) : __builtin_amdgcn_readlane(__float_as_int(u[1]), j - 64));
+            if (same) sum[h] += uj;
+            if (same && j < lane + 64 * h) first[h] = false;
+        });
+    }
+    const float uh = ENT ? p.up_entropy[r] : 0.f, logs = p.stats[2 * r + 1];
+    Slope<Val> f;
+    f.m = of_bits<Val>(p.stats[2 * r]);
+    f.l2 = logs * LOG2E;
+    f.a0 = -p.l.scale * (up + (uh != 0.f ? uh * p.entropy[r] : 0.f));
+    f.a1 = -p.l.scale * uh * LN2;
+    f.zero = !(__any(named.c[0] >= 0 || named.c[1] >= 0) || uh != 0.f) || logs == NEG_INF;
+    store_gradient<TYPE, NV, ENT>(p, r, chunk, f, named, first, raw, [&](int h, Val v, auto value) { return value(v) + p.l.scale * sum[h]; });
+}
 
+// w scale (Q p_j - sum of the q of j), and with the rest class for those that are no entry w scale (p_j / p_rest) (Q p_rest - q_rest)
+template <int TYPE, int NV>
+__global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillParams p) {
+    using Val = typename Kind<TYPE>::Val;
+    const uint32_t row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks, lane = threadIdx.x & 63;
+    const uint64_t r = p.row0 + row;
+    uint4 raw[NV];
+    load_chunk<TYPE, NV>(p, r, chunk, raw);
+    const DistillStat st = *(const DistillStat *)(p.stats + 8 * r);
+    const float w = p.weight ? p.weight[r] : 1.f, c = p.l.scale * LOG2E;
+    Named named;
+    named.load(p.entry + r * p.top, p.top);
+    const Val m = of_bits<Val>(st.m), rest_m = of_bits<Val>(st.rest_m);
+    Slope<Val> f;
+    f.zero = w == 0.f || st.logs == NEG_INF;
+    f.a0 = p.l.scale * w * st.total;
+    f.a1 = 0.f;
+    f.m = m;
+    f.l2 = st.logs * LOG2E;
+    if (p.rest) {
+        const bool none = st.rest_logs == NEG_INF;   // no possible class outside the entries: their gradient is 0 by 2^d alone
+        f.a0 = p.l.scale * w * (none ? -st.left : st.total * expf(p.l.scale * below(rest_m, m) + st.rest_logs - st.logs) - st.left);
+        f.m = rest_m;
+        f.l2 = none ? 0.f : st.rest_logs * LOG2E;
+        if (st.total != st.total) f.a0 = st.total;
+    }
+    float q[2], sum[2] = {};
+    bool first[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        q[h] = named.c[h] >= 0 ? expf(p.value_scale * (teacher_value(p.value, p.value_type, r * p.top + lane + 64 * h) - st.value_m) - st.value_logs) : 0.f;
+        first[h] = named.c[h] >= 0;
+    }
+    named.pairs(p.top, [&](int h, uint32_t j, bool same) {
+        const float qj = __int_as_float(j < 64 ? __builtin_amdgcn_readlane(__float_as_int(q[0]), j) : __builtin_amdgcn_readlane(__float_as_int(q[1]), j - 64));
+        if (same) sum[h] += qj;
+        if (same && j < lane + 64 * h) first[h] = false;
+    });
+    store_gradient<TYPE, NV, false>(p, r, chunk, f, named, first, raw, [&](int h, Val v, auto) {
+        return p.l.scale * w * (st.total * __builtin_amdgcn_exp2f(c * below(v, m) - st.logs * LOG2E) - sum[h]);
+    });
+}
 
 // ---- launches ------------------------------------------------------------------------
 
@@ -665,27 +827,96 @@ RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top) {
     return cut;
 }
 
-hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st) {
+template <class Params>
+static void set_cut(Params &p, const RowCut &cut) {
     p.chunks = cut.chunks;
     p.chunk_vecs = cut.chunk_vecs;
-    p.list_cap = cut.list_cap;
-    p.parts = (Part *)workspace;
-    p.lists = (uint2 *)((uint8_t *)workspace + cut.parts_bytes);
+}
+
+// launch(rows) for the runs of rows that a launch takes
+template <class Params, class Launch>
+static hipError_t by_runs(Params &p, const RowCut &cut, Launch launch) {
     for (p.row0 = 0; p.row0 < p.l.rows; p.row0 += cut.rows) {
-        const uint32_t rows = (uint32_t)std::min<uint64_t>(cut.rows, p.l.rows - p.row0);
-        switch (p.l.type) {
-        case ISR_F32: launch_rows<ISR_F32>(p, cut.nv, rows, st); break;
-        case ISR_BF16: launch_rows<ISR_BF16>(p, cut.nv, rows, st); break;
-        case ISR_F16: launch_rows<ISR_F16>(p, cut.nv, rows, st); break;
-        default: launch_rows<ISR_I32>(p, cut.nv, rows, st); break;
-        }
+        launch((uint32_t)std::min<uint64_t>(cut.rows, p.l.rows - p.row0));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
-hipError_t launch_logprobs_grad(const LogprobsGradParams &p, hipStream_t st) { LAUNCH_BY_TYPE(logprobs_grad_kernel, p, st); }
-hipError_t launch_distill(const DistillParams &p, hipStream_t st) { LAUNCH_BY_TYPE(distill_kernel, p, st); }
-hipError_t launch_distill_grad(const DistillParams &p, hipStream_t st) { LAUNCH_BY_TYPE(distill_grad_kernel, p, st); }
+
+#define BY_TYPE(type, call)                          \
+    switch (type) {                                  \
+    case ISR_F32: call(ISR_F32); break;              \
+    case ISR_BF16: call(ISR_BF16); break;            \
+    case ISR_F16: call(ISR_F16); break;              \
+    default: call(ISR_I32); break;                   \
+    }
+
+hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st) {
+    set_cut(p, cut);
+    p.list_cap = cut.list_cap;
+    p.parts = (Part *)workspace;
+    p.lists = (uint2 *)((uint8_t *)workspace + cut.parts_bytes);
+    return by_runs(p, cut, [&](uint32_t rows) {
+#define CALL(T) launch_rows<T>(p, cut.nv, rows, st)
+        BY_TYPE(p.l.type, CALL)
+#undef CALL
+    });
+}
+
+template <int TYPE>
+static void launch_distill_rows(const DistillParams &p, uint32_t nv, uint32_t rows, hipStream_t st) {
+    const dim3 grid(rows * p.chunks), block(THREADS);
+    if (p.rest && nv == 2) hipLaunchKernelGGL((distill_kernel<TYPE, 2, true>), grid, block, 0, st, p);
+    else if (p.rest) hipLaunchKernelGGL((distill_kernel<TYPE, 8, true>), grid, block, 0, st, p);
+    else if (nv == 2) hipLaunchKernelGGL((distill_kernel<TYPE, 2, false>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((distill_kernel<TYPE, 8, false>), grid, block, 0, st, p);
+    if (p.chunks > 1) hipLaunchKernelGGL((distill_join_kernel<TYPE>), dim3(rows), block, 0, st, p);
+}
+
+hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st) {
+    set_cut(p, cut);
+    p.parts = (Part *)workspace;
+    return by_runs(p, cut, [&](uint32_t rows) {
+#define CALL(T) launch_distill_rows<T>(p, cut.nv, rows, st)
+        BY_TYPE(p.l.type, CALL)
+#undef CALL
+    });
+}
+
+// Gradients keep less of a row in registers: nothing is exchanged between threads but the named classes.
+static RowCut cut_gradient(const LogitRows &l) {
+    RowCut cut{};
+    const uint32_t per_vec = l.type == ISR_F32 || l.type == ISR_I32 ? 4 : 8, vecs = l.classes / per_vec;
+    cut.nv = 4;
+    cut.chunks = vecs <= 4 * THREADS ? 1 : (vecs + 4 * THREADS - 1) / (4 * THREADS);
+    cut.chunk_vecs = vecs ? (vecs + cut.chunks - 1) / cut.chunks : 1;
+    const uint64_t most = (1u << 22) / cut.chunks;
+    cut.rows = (uint32_t)std::min<uint64_t>(l.rows, most ? most : 1);
+    return cut;
+}
+
+hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st) {
+    const RowCut cut = cut_gradient(p.l);
+    set_cut(p, cut);
+    return by_runs(p, cut, [&](uint32_t rows) {
+        const dim3 grid(rows * p.chunks), block(THREADS);
+#define CALL(T)                                                                                             \
+    if (p.up_entropy) hipLaunchKernelGGL((logprobs_grad_kernel<T, 4, true>), grid, block, 0, st, p);        \
+    else hipLaunchKernelGGL((logprobs_grad_kernel<T, 4, false>), grid, block, 0, st, p)
+        BY_TYPE(p.l.type, CALL)
+#undef CALL
+    });
+}
+
+hipError_t launch_distill_grad(DistillParams p, hipStream_t st) {
+    const RowCut cut = cut_gradient(p.l);
+    set_cut(p, cut);
+    return by_runs(p, cut, [&](uint32_t rows) {
+#define CALL(T) hipLaunchKernelGGL((distill_grad_kernel<T, 4>), dim3(rows * p.chunks), dim3(THREADS), 0, st, p)
+        BY_TYPE(p.l.type, CALL)
+#undef CALL
+    });
+}
 
 }  // namespace isr
