@@ -139,9 +139,7 @@ int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weig
     const RowCut cut = cut_rows(l->type, l->classes, l->rows, 0);
     float *stats = stats_device || !grad_logits_device ? stats_device : (float *)((uint8_t *)workspace_device + cut.parts_bytes);
     const DistillParams p = distill_params(l, t, row_weight_device, loss_device, stats, grad_logits_device, grad_row_stride);
-    hipError_t e = launch_distill(p, cut, workspace_device, (hipStream_t)hip_stream);
-    if (e == hipSuccess && grad_logits_device) e = launch_distill_grad(p, (hipStream_t)hip_stream);
-    return status(e);
+    return status(launch_distill(p, cut, workspace_device, (hipStream_t)hip_stream));
 }
 
 int isr_distill_grad(const isr_logits *l, const isr_teacher *t, const float *row_weight_device, const float *stats_device,

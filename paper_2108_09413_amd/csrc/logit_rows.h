@@ -70,7 +70,7 @@ struct DistillParams {
 
 hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st);
 hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st);
-hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st);
+hipError_t launch_distill(DistillParams p, RowCut cut, void *workspace, hipStream_t st);   // and the gradient, if p.grad
 hipError_t launch_distill_grad(DistillParams p, hipStream_t st);
 
 }  // namespace isr

@@ -81,9 +81,17 @@ __device__ __forceinline__ float wave_sum(float v) { return wave_fold(v, [](floa
 __device__ __forceinline__ int wave_sum(int v) { return wave_fold(v, [](int a, int b) { return a + b; }); }
 template <class T> __device__ __forceinline__ T wave_max(T v) { return wave_fold(v, [](T a, T b) { return larger(a, b); }); }
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    auto add = [&](auto of) {
+        const int2 b = __builtin_bit_cast(int2, v);
+        v += __builtin_bit_cast(double, make_int2(of(b.x), of(b.y)));
+    };
+    add([](int b) { return dpp<0xB1>(b); });
+    add([](int b) { return dpp<0x4E>(b); });
+    add([](int b) { return dpp<0x141>(b); });
+    add([](int b) { return dpp<0x140>(b); });
+    const int2 b = __builtin_bit_cast(int2, v);
+    auto at = [&](int lane) { return __builtin_bit_cast(double, make_int2(__builtin_amdgcn_readlane(b.x, lane), __builtin_amdgcn_readlane(b.y, lane))); };
+    return (at(0) + at(16)) + (at(32) + at(48));
 }
 
 template <class Val>
@@ -236,25 +244,53 @@ struct Part {
     uint32_t listed;
 };
 
-// Results of a row of logits, by the whole workgroup.  The list is complete.
+// Results of a row of logits, by its workgroup.
+template <class Val>
+struct Logp {
+    float scale, logs;
+    Val m;
+    bool bad, empty;
+    __device__ __forceinline__ Logp(const LogitRows &l, const Stat<Val> &a) : scale(l.scale), logs(a.s == 0.f ? 0.f : logf(a.s)), m(a.m), bad(a.s != a.s), empty(a.s == 0.f) {}
+    __device__ __forceinline__ float operator()(Val v) const { return bad ? __builtin_nanf("") : possible(v) ? scale * below(v, m) - logs : NEG_INF; }
+};
+
+// The given classes, one a thread of the first 64 or 128, read ahead of what their results wait for.
 template <int TYPE>
-__device__ void finish_logprobs(const LogprobsParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a, Shared &sh) {
-    using K = Kind<TYPE>;
-    using Val = typename K::Val;
-    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
-    const bool bad = a.s != a.s, empty = a.s == 0.f;
-    const float logs = empty ? 0.f : logf(a.s), nan = __builtin_nanf("");
-    auto logp = [&](Val v) { return bad ? nan : possible(v) ? p.l.scale * below(v, a.m) - logs : NEG_INF; };
+struct Given {
+    int32_t c[2];
+    typename Kind<TYPE>::Val at[2];
+    __device__ __forceinline__ void load(const LogprobsParams &p, uint64_t r) {
+        const auto *x = (const typename Kind<TYPE>::Raw *)p.l.x + r * p.l.stride;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t g = threadIdx.x + h * blockDim.x;
+            c[h] = g < p.n_given ? p.given[r * p.n_given + g] : -1;
+            at[h] = (uint32_t)c[h] < p.l.classes ? Kind<TYPE>::val(x[c[h]]) : lowest(typename Kind<TYPE>::Val());
+        }
+    }
+};
+
+template <int TYPE>
+__device__ __forceinline__ void finish_values(const LogprobsParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a, const Given<TYPE> &given) {
+    const Logp<typename Kind<TYPE>::Val> logp(p.l, a);
+    const float nan = __builtin_nanf("");
     if (threadIdx.x == 0) {
-        if (p.entropy) p.entropy[r] = bad ? nan : empty ? 0.f : logs - LN2 * (a.t / a.s);
-        if (p.stats) { p.stats[2 * r] = bits_of(a.m); p.stats[2 * r + 1] = bad ? nan : empty ? NEG_INF : logs; }
+        if (p.entropy) p.entropy[r] = logp.bad ? nan : logp.empty ? 0.f : logp.logs - LN2 * (a.t / a.s);
+        if (p.stats) { p.stats[2 * r] = bits_of(a.m); p.stats[2 * r + 1] = logp.bad ? nan : logp.empty ? NEG_INF : logp.logs; }
     }
-    if (threadIdx.x < p.n_given) {
-        const int32_t c = p.given[r * p.n_given + threadIdx.x];
-        p.logprob[r * p.n_given + threadIdx.x] = c < 0 ? 0.f : (uint32_t)c < p.l.classes ? logp(K::val(x[c])) : nan;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t g = threadIdx.x + h * blockDim.x;
+        if (g < p.n_given) p.logprob[r * p.n_given + g] = given.c[h] < 0 ? 0.f : (uint32_t)given.c[h] < p.l.classes ? logp(given.at[h]) : nan;
     }
-    if (p.top == 0) return;
-    const uint32_t n = bad ? 0 : min(sh.listed, (uint32_t)LIST);
+}
+
+// The list is complete.
+template <int TYPE>
+__device__ __forceinline__ void finish_top(const LogprobsParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a, Shared &sh) {
+    using Val = typename Kind<TYPE>::Val;
+    const Logp<Val> logp(p.l, a);
+    const uint32_t n = logp.bad ? 0 : min(sh.listed, (uint32_t)LIST);
     for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
         const uint2 mine = sh.list[i];
         const uint64_t own = (uint64_t)mine.x << 32 | mine.y;
@@ -271,7 +307,7 @@ __device__ void finish_logprobs(const LogprobsParams &p, uint64_t r, const Stat<
     }
     for (uint32_t k = n + threadIdx.x; k < p.top; k += THREADS) {
         p.top_class[r * p.top + k] = -1;
-        p.top_logprob[r * p.top + k] = bad ? nan : NEG_INF;
+        p.top_logprob[r * p.top + k] = logp.bad ? __builtin_nanf("") : NEG_INF;
     }
 }
 
@@ -294,6 +330,8 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
         for (int i = 0; i < NV; ++i) raw[i] = ((const Loose *)(x + (size_t)(v0 + min(i * THREADS + tid, n - 1)) * PV))->v;
     }
     const Val edge = tail ? K::val(x[rest]) : lowest(Val());
+    Given<TYPE> given;
+    if (p.chunks == 1) given.load(p, r);
     Stat<Val> a{edge, 0.f, 0.f};
     if (TOP && tid == 0) sh.listed = 0;
 #pragma unroll
@@ -353,7 +391,8 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
         }
     }
     if (p.chunks == 1) {
-        finish_logprobs<TYPE>(p, r, all, sh);
+        finish_values<TYPE>(p, r, all, given);
+        if constexpr (TOP) finish_top<TYPE>(p, r, all, sh);
         return;
     }
     const size_t at = (size_t)row * p.chunks + chunk;
@@ -362,11 +401,12 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
         for (uint32_t i = tid; i < sh.listed; i += THREADS) p.lists[at * p.list_cap + i] = sh.list[i];
 }
 
-// The chunks of a row together.
+// The chunks of a row together, by one wave.
 template <class Val>
-__device__ __forceinline__ Stat<Val> join_parts(const Part *parts, uint32_t chunks, float c, SharedStat &sh) {
+__device__ __forceinline__ Stat<Val> join_parts(const Part *parts, uint32_t chunks, float c) {
+    const uint32_t lane = threadIdx.x & 63;
     Stat<Val> a{lowest(Val()), 0.f, 0.f};
-    for (uint32_t i = threadIdx.x; i < chunks; i += THREADS) {
+    for (uint32_t i = lane; i < chunks; i += 64) {
         const Part q = parts[i];
         const Val qm = __builtin_bit_cast(Val, q.m), m = larger(a.m, qm);
         const float d0 = c * below(a.m, m), d1 = c * below(qm, m), f0 = __builtin_amdgcn_exp2f(d0), f1 = __builtin_amdgcn_exp2f(d1);
@@ -374,46 +414,79 @@ __device__ __forceinline__ Stat<Val> join_parts(const Part *parts, uint32_t chun
         const float s1 = q.s == 0.f ? 0.f : f1 * q.s, t1 = q.s == 0.f ? 0.f : f1 * (q.t + fmaxf(d1, NO_SHARE) * q.s);
         a = {m, s0 + s1, t0 + t1};
     }
-    return block_stat(a, c, sh, [] {});
+    const Val m = wave_max(a.m);
+    const float d = c * below(a.m, m), f = __builtin_amdgcn_exp2f(d);
+    return {m, wave_sum(a.s == 0.f ? 0.f : f * a.s), wave_sum(a.s == 0.f ? 0.f : f * (a.t + fmaxf(d, NO_SHARE) * a.s))};
 }
 
-template <int TYPE, bool TOP>
-__global__ __launch_bounds__(THREADS) void logprobs_join_kernel(const LogprobsParams p) {
+// Without top alternatives a wave a row, with them a workgroup.
+template <int TYPE>
+__global__ __launch_bounds__(64) void logprobs_join_kernel(const LogprobsParams p) {
+    using Val = typename Kind<TYPE>::Val;
+    Given<TYPE> given;
+    given.load(p, p.row0 + blockIdx.x);
+    const Stat<Val> all = join_parts<Val>(p.parts + (size_t)blockIdx.x * p.chunks, p.chunks, p.l.scale * LOG2E);
+    finish_values<TYPE>(p, p.row0 + blockIdx.x, all, given);
+}
+
+// FEW: at most 16 lists of at most 128: everything is read at once, the lists as far as they have room, and kept.
+template <int TYPE, bool FEW>
+__global__ __launch_bounds__(THREADS) void logprobs_top_join_kernel(const LogprobsParams p) {
     using Val = typename Kind<TYPE>::Val;
     __shared__ __attribute__((aligned(16))) Shared sh;
-    const uint32_t tid = threadIdx.x, row = blockIdx.x;
+    const uint32_t tid = threadIdx.x, row = blockIdx.x, lane = tid & 63, wave = tid >> 6;
     const Part *parts = p.parts + (size_t)row * p.chunks;
-    const Stat<Val> all = join_parts<Val>(parts, p.chunks, p.l.scale * LOG2E, sh);
-    if constexpr (TOP) {
-        const uint2 *lists = p.lists + (size_t)row * p.chunks * p.list_cap;
-        auto each = [&](auto f) {   // a wave a list
-            for (uint32_t q = tid >> 6; q < p.chunks; q += THREADS / 64) {
+    const uint2 *lists = p.lists + (size_t)row * p.chunks * p.list_cap;
+    Given<TYPE> given;
+    given.load(p, p.row0 + row);
+    uint2 kept[FEW ? 8 : 1];
+    if constexpr (FEW) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t q = wave + 4 * (i >> 1), at = lane + 64 * (i & 1);
+            kept[i] = q < p.chunks && at < p.list_cap ? lists[(size_t)q * p.list_cap + at] : make_uint2(0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t q = wave + 4 * (i >> 1), at = lane + 64 * (i & 1);
+            if (q >= p.chunks || at >= parts[q].listed) kept[i] = make_uint2(0, 0);   // less than any key of a possible class
+        }
+    }
+    auto each = [&](auto f) {   // a wave a list
+        if constexpr (FEW) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (kept[i].y) f(kept[i].x, ~kept[i].y);
+        } else {
+            for (uint32_t q = wave; q < p.chunks; q += THREADS / 64) {
                 const uint32_t n = parts[q].listed;
-                for (uint32_t i = tid & 63; i < n; i += 64) {
+                for (uint32_t i = lane; i < n; i += 64) {
                     const uint2 w = lists[(size_t)q * p.list_cap + i];
                     f(w.x, ~w.y);
                 }
             }
-        };
-        uint32_t best = 0;
-        each([&](uint32_t key, uint32_t) { best = max(best, key); });
-        sh.key[tid] = best;
-        if (tid == 0) sh.listed = 0;
-        __syncthreads();
-        const uint32_t bound = key_bound<LOW_BITS<Val>>(sh, p.top);
-        each([&](uint32_t key, uint32_t cls) {
-            if (key >= bound) {
-                const uint32_t at = atomicAdd(&sh.listed, 1u);
-                if (at < LIST) sh.list[at] = make_uint2(key, ~cls);
-            }
-        });
-        __syncthreads();
-        if (sh.listed > LIST) {
-            __syncthreads();
-            list_exactly(each, p.top, sh);
         }
+    };
+    uint32_t best = 0;
+    each([&](uint32_t key, uint32_t) { best = max(best, key); });
+    sh.key[tid] = best;
+    if (tid == 0) sh.listed = 0;
+    const Stat<Val> all = join_parts<Val>(parts, p.chunks, p.l.scale * LOG2E);   // every wave for itself
+    __syncthreads();
+    const uint32_t bound = key_bound<LOW_BITS<Val>>(sh, p.top);
+    each([&](uint32_t key, uint32_t cls) {
+        if (key >= bound) {
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at < LIST) sh.list[at] = make_uint2(key, ~cls);
+        }
+    });
+    __syncthreads();
+    if (sh.listed > LIST) {
+        __syncthreads();
+        list_exactly(each, p.top, sh);
     }
-    finish_logprobs<TYPE>(p, p.row0 + row, all, sh);
+    finish_values<TYPE>(p, p.row0 + row, all, given);
+    finish_top<TYPE>(p, p.row0 + row, all, sh);
 }
 
 // ---- distillation -----------------------------------------------------------------------
@@ -443,67 +516,110 @@ struct Named {
             c[h] = i < n ? p[i] : -1;
         }
     }
-    // visit(h, j, same): for each of the lane's two and each j < n in ascending order, whether they name one class
+    // visit(j, class) in ascending order for the indexes whose bit is set in `of`
     template <class Visit>
-    __device__ __forceinline__ void pairs(uint32_t n, Visit visit) const {
-        for (uint32_t j = 0; j < n; ++j) {
-            const int other = j < 64 ? __builtin_amdgcn_readlane(c[0], j) : __builtin_amdgcn_readlane(c[1], j - 64);
-            visit(0, j, other == c[0]);
-            if (n > 64) visit(1, j, other == c[1]);
+    __device__ __forceinline__ void visit(const uint64_t (&of)[2], Visit f) const {
+        for (uint64_t left = of[0]; left; left &= left - 1) {
+            const int j = __builtin_ctzll(left);
+            f(j, __builtin_amdgcn_readlane(c[0], j));
+        }
+        for (uint64_t left = of[1]; left; left &= left - 1) {
+            const int j = __builtin_ctzll(left);
+            f(j + 64, __builtin_amdgcn_readlane(c[1], j));
         }
     }
-    // whether the class is the first of its name
-    __device__ __forceinline__ void first(uint32_t n, bool (&is)[2]) const {
-        const uint32_t lane = threadIdx.x & 63;
-        is[0] = c[0] >= 0;
-        is[1] = c[1] >= 0;
-        pairs(n, [&](int h, uint32_t j, bool same) { if (same && j < lane + 64 * h) is[h] = false; });
+    // of the indexes in `of`, those whose class an earlier one of them has
+    __device__ __forceinline__ void repeated(const uint64_t (&of)[2], uint64_t (&again)[2]) const {
+        again[0] = again[1] = 0;
+        visit(of, [&](int j, int cls) {
+            const uint64_t same0 = __ballot(c[0] == cls), same1 = __ballot(c[1] == cls);
+            if (j < 64) {
+                again[0] |= same0 & (~1ull << j);
+                again[1] |= same1;
+            } else {
+                again[1] |= same1 & (~1ull << (j - 64));
+            }
+        });
+    }
+};
+constexpr int SLOTS = 2048;
+__device__ __forceinline__ bool lane_of(uint64_t bits) { return bits >> (threadIdx.x & 63) & 1; }
+
+// Loss and statistics of a row, by one wave, from the statistics of all classes or (rest) of those that are no entry.  The sums
+// over the entries are in 64 bits: q_rest is next to 0 where the entries hold nearly all, and the loss of a student close to its
+// teacher is a sum that cancels.
+template <int TYPE>
+struct Entries : Named {
+    float v[2];                      // the teacher's
+    typename Kind<TYPE>::Val at[2];  // the student's
+    __device__ __forceinline__ void load(const DistillParams &p, uint64_t r) {
+        const auto *x = (const typename Kind<TYPE>::Raw *)p.l.x + r * p.l.stride;
+        Named::load(p.entry + r * p.top, p.top);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v[h] = c[h] >= 0 ? teacher_value(p.value, p.value_type, r * p.top + (threadIdx.x & 63) + 64 * h) : NEG_INF;
+            at[h] = (uint32_t)c[h] < p.l.classes ? Kind<TYPE>::val(x[c[h]]) : lowest(typename Kind<TYPE>::Val());   // not negative either
+        }
     }
 };
 
-// Loss and statistics of a row, by one wave, from the statistics of all classes or (rest) of those that are no entry.  A few
-// hundred operations a row, in 64 bits: q_rest is next to 0 where the entries hold nearly all, and the loss of a student close
-// to its teacher is a sum that cancels.
-template <int TYPE>
-__device__ void finish_distill(const DistillParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a) {
-    using K = Kind<TYPE>;
-    using Val = typename K::Val;
-    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+// Which of a row's entries are the first of their class, by one wave.  The lowest index of those that fall on one slot of a table
+// knows about itself and all of its class; only entries that find another class there (2 of 64 on average) are gone through in
+// turn.  All in turn took 3 us a row of 64.
+__device__ __forceinline__ void first_entries(const Named &e, uint32_t *table, bool (&is)[2]) {
     const uint32_t lane = threadIdx.x & 63;
-    Named e;
-    e.load(p.entry + r * p.top, p.top);
-    float v[2];
+    auto ordered = [] {   // within the wave
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        __builtin_amdgcn_wave_barrier();
+    };
+#pragma unroll
+    for (int i = 0; i < SLOTS / 256; ++i) ((uint4 *)table)[i * 64 + lane] = make_uint4(~0u, ~0u, ~0u, ~0u);
+    ordered();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (e.c[h] >= 0) atomicMin(&table[e.c[h] % SLOTS], lane + 64 * h);
+    ordered();
+    bool other[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t j = e.c[h] >= 0 ? table[e.c[h] % SLOTS] : lane + 64 * h;
+        const int c0 = __shfl(e.c[0], j & 63, 64), c1 = __shfl(e.c[1], j & 63, 64);
+        other[h] = e.c[h] >= 0 && (j < 64 ? c0 : c1) != e.c[h];
+        is[h] = e.c[h] >= 0 && j == lane + 64 * h;
+    }
+    const uint64_t of[2] = {__ballot(other[0]), __ballot(other[1])};
+    uint64_t again[2];
+    e.repeated(of, again);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (other[h]) is[h] = !lane_of(again[h]);
+}
+
+template <int TYPE>
+__device__ DistillStat finish_distill(const DistillParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a, const Entries<TYPE> &e, uint32_t *table) {
+    using Val = typename Kind<TYPE>::Val;
+    const Val (&at)[2] = e.at;
     bool bad = false;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        v[h] = e.c[h] >= 0 ? teacher_value(p.value, p.value_type, r * p.top + lane + 64 * h) : NEG_INF;
-        bad |= e.c[h] >= 0 && ((uint32_t)e.c[h] >= p.l.classes || v[h] != v[h] || v[h] == -NEG_INF);
-    }
-    const bool any = __any(e.c[0] >= 0 || e.c[1] >= 0);
+    for (int h = 0; h < 2; ++h) bad |= e.c[h] >= 0 && ((uint32_t)e.c[h] >= p.l.classes || e.v[h] != e.v[h] || e.v[h] == -NEG_INF);
     bad = __any(bad);
-    const float vm = p.rest ? 0.f : wave_max(larger(v[0], v[1]));
-    if (!any || vm == NEG_INF) {
-        if (lane == 0) {
-            p.loss[r] = 0.f;
-            if (p.stats) *(DistillStat *)(p.stats + 8 * r) = DistillStat{0.f, NEG_INF, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        }
-        return;
+    const float vm = p.rest ? 0.f : wave_max(larger(e.v[0], e.v[1])), c = p.l.scale * LOG2E;
+    if (!__any(e.c[0] >= 0 || e.c[1] >= 0) || vm == NEG_INF) {
+        if ((threadIdx.x & 63) == 0) p.loss[r] = 0.f;
+        return DistillStat{0.f, NEG_INF, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     }
-    const float c = p.l.scale * LOG2E;
-    double lq[2], q[2];
-    Val at[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        lq[h] = (double)p.value_scale * ((double)v[h] - vm);
-        q[h] = exp(lq[h]);
-        at[h] = e.c[h] >= 0 && (uint32_t)e.c[h] < p.l.classes ? K::val(x[e.c[h]]) : lowest(Val());
-    }
-    double total = wave_sum(q[0] + q[1]), value_logs = 0.0, left = 0.0;
+    double lq[2], q[2], total, left = 0.0;
+    float value_logs = 0.f;
     Stat<Val> all = a;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) lq[h] = (double)p.value_scale * ((double)e.v[h] - vm);
     if (p.rest) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) q[h] = e.c[h] >= 0 ? exp(lq[h]) : 0.0;
+        total = wave_sum(q[0] + q[1]);
         left = fmax(1.0 - total, 0.0);
         bool is[2];
-        e.first(p.top, is);
+        first_entries(e, table, is);
         all.m = larger(a.m, wave_max(larger(is[0] ? at[0] : lowest(Val()), is[1] ? at[1] : lowest(Val()))));
         float s = 0.f;
 #pragma unroll
@@ -511,31 +627,38 @@ __device__ void finish_distill(const DistillParams &p, uint64_t r, const Stat<ty
             if (is[h]) s += __builtin_amdgcn_exp2f(c * below(at[h], all.m));
         all.s = wave_sum(s) + (a.s == 0.f ? 0.f : a.s * __builtin_amdgcn_exp2f(c * below(a.m, all.m)));
     } else {
-        value_logs = log(total);
-        total = 0.0;
+        float z = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) z += e.c[h] >= 0 ? expf((float)lq[h]) : 0.f;
+        value_logs = logf(wave_sum(z));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            lq[h] -= value_logs;
+            q[h] = e.c[h] >= 0 ? expf((float)lq[h]) : 0.f;
+        }
+        total = wave_sum(q[0] + q[1]);
     }
     const bool empty = all.s == 0.f;
-    const double logs = empty ? 0.0 : log((double)all.s), rest_logs = a.s == 0.f ? (double)NEG_INF : log((double)a.s);
+    const float logs = empty ? 0.f : logf(all.s), rest_logs = a.s == 0.f ? NEG_INF : logf(a.s);
     double loss = 0.0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        if (!p.rest) { lq[h] -= value_logs; q[h] = exp(lq[h]); total += q[h]; }
         const double lp = empty || !possible(at[h]) ? (double)NEG_INF : (double)p.l.scale * below64(at[h], all.m) - logs;
-        if (e.c[h] >= 0 && q[h] > 0.0) loss += q[h] * (lq[h] - lp);
+        if (q[h] > 0.0) loss += q[h] * (lq[h] - lp);
     }
     loss = wave_sum(loss);
-    if (!p.rest) total = wave_sum(total);
     if (left > 0.0) {
-        const double lr = a.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(a.m, all.m) + rest_logs - logs;
-        loss += left * (log(left) - lr);
+        const double lr = a.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(a.m, all.m) + ((double)rest_logs - logs);
+        loss += left * (logf((float)left) - lr);
     }
     total += left;
     if (bad || all.s != all.s) loss = total = __builtin_nan("");
-    if (lane != 0) return;
-    p.loss[r] = (float)loss;
-    if (p.stats)
-        *(DistillStat *)(p.stats + 8 * r) = DistillStat{bits_of(all.m), empty ? NEG_INF : (float)logs, bits_of(a.m), (float)rest_logs,
-                                                         vm, (float)value_logs, (float)total, (float)left};
+    if ((threadIdx.x & 63) == 0) p.loss[r] = (float)loss;
+    return DistillStat{bits_of(all.m), empty ? NEG_INF : logs, bits_of(a.m), rest_logs, vm, value_logs, (float)total, (float)left};
+}
+
+__device__ __forceinline__ void store_stat(const DistillParams &p, uint64_t r, const DistillStat &st) {
+    if (p.stats && (threadIdx.x & 63) == 0) *(DistillStat *)(p.stats + 8 * r) = st;
 }
 
 // The chunk of a row as in logprobs_kernel.  REST: without the entries, which a byte of bits for each vector in LDS tells: a
@@ -547,6 +670,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p)
     constexpr int PV = PER_VEC<TYPE>;
     __shared__ SharedStat sh;
     __shared__ __attribute__((aligned(8))) uint32_t mask[REST ? NV * THREADS / 4 : 1];
+    __shared__ __attribute__((aligned(16))) uint32_t table[REST ? SLOTS : 4];
     __shared__ uint32_t tail_mask;
     const uint32_t tid = threadIdx.x, row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks;
     const uint64_t r = p.row0 + row;
@@ -554,6 +678,8 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p)
     const uint32_t vecs = p.l.classes / PV, v0 = chunk * p.chunk_vecs, n = min(p.chunk_vecs, vecs - min(vecs, v0));
     const uint32_t rest = vecs * PV + tid;
     bool tail = chunk == p.chunks - 1 && rest < p.l.classes;
+    // in front of the row's loads, which would have to arrive first otherwise
+    const int32_t e = REST && tid < p.top ? p.entry[r * p.top + tid] : -1;
     uint4 raw[NV];
     if (n) {
 #pragma unroll
@@ -564,7 +690,6 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p)
     if constexpr (REST) {
         for (int i = tid; i < NV * THREADS / 4; i += THREADS) mask[i] = 0;
         if (tid == 0) tail_mask = 0;
-        const int32_t e = tid < p.top ? p.entry[r * p.top + tid] : -1;
         __syncthreads();
         const uint32_t j = (uint32_t)e - v0 * PV;
         if (e >= 0 && (uint32_t)e >= v0 * PV && j < n * PV) {
@@ -616,25 +741,32 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p)
     }
     const Stat<Val> all = block_stat(a, c, sh, [] {});
     if (p.chunks == 1) {
-        if (tid < 64) finish_distill<TYPE>(p, r, all);
+        if (tid < 64) {
+            Entries<TYPE> named;
+            named.load(p, r);
+            store_stat(p, r, finish_distill<TYPE>(p, r, all, named, table));
+        }
         return;
     }
     if (tid == 0) p.parts[(size_t)row * p.chunks + chunk] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, 0.f, 0};
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(THREADS) void distill_join_kernel(const DistillParams p) {
+__global__ __launch_bounds__(64) void distill_join_kernel(const DistillParams p) {
     using Val = typename Kind<TYPE>::Val;
-    __shared__ SharedStat sh;
-    const Stat<Val> all = join_parts<Val>(p.parts + (size_t)blockIdx.x * p.chunks, p.chunks, p.l.scale * LOG2E, sh);
-    if (threadIdx.x < 64) finish_distill<TYPE>(p, p.row0 + blockIdx.x, all);
+    __shared__ __attribute__((aligned(16))) uint32_t table[SLOTS];
+    const uint64_t r = p.row0 + blockIdx.x;
+    Entries<TYPE> named;
+    named.load(p, r);
+    const Stat<Val> all = join_parts<Val>(p.parts + (size_t)blockIdx.x * p.chunks, p.chunks, p.l.scale * LOG2E);
+    store_stat(p, r, finish_distill<TYPE>(p, r, all, named, table));
 }
 
 // ---- gradients --------------------------------------------------------------------------
 
 // A chunk of a gradient's row: with d = c (x - m) - l2 the log2 of a probability, every element gets 2^d (a0 + a1 d), and the
-// named classes what `special(h, x)` says of them.  Their logits are read before anything is stored (the gradient may go
-// over the logits) and theirs is stored behind all others' (a barrier each, in chunks that hold one).
+// named classes what `special` says of them, from their logit and the sum of `part(h)` over the names of one class.
+// Wave 0 stores theirs behind a barrier; where the gradient goes over the logits it reads them in front of another.
 template <class Val>
 struct Slope {
     Val m;
@@ -642,9 +774,9 @@ struct Slope {
     bool zero;   // the row's gradient is zero
 };
 
-template <int TYPE, int NV, bool LINEAR, class Params, class Special>
+template <int TYPE, int NV, bool LINEAR, class Params, class Part, class Special>
 __device__ __forceinline__ void store_gradient(const Params &p, uint64_t r, uint32_t chunk, const Slope<typename Kind<TYPE>::Val> &f, const Named &named,
-                                               const bool (&first)[2], const uint4 (&raw)[NV], Special special) {
+                                               const uint4 (&raw)[NV], Part part, Special special) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>;
@@ -659,18 +791,32 @@ __device__ __forceinline__ void store_gradient(const Params &p, uint64_t r, uint
         const float d = c * below(v, f.m) - f.l2, e = __builtin_amdgcn_exp2f(d);
         return LINEAR ? e * (f.a0 + f.a1 * fmaxf(d, NO_SHARE)) : e * f.a0;
     };
-    bool here[2];
-    float own[2] = {};
+    uint64_t here[2];   // the names in this chunk, the same in every wave
 #pragma unroll
-    for (int h = 0; h < 2; ++h) here[h] = !f.zero && named.c[h] >= 0 && (uint32_t)named.c[h] >= lo && (uint32_t)named.c[h] < hi;
-    const bool some = __any(here[0] || here[1]);   // the same in every wave
+    for (int h = 0; h < 2; ++h) here[h] = f.zero ? 0 : __ballot(named.c[h] >= 0 && (uint32_t)named.c[h] >= lo && (uint32_t)named.c[h] < hi);
+    const bool some = (here[0] | here[1]) != 0, over = p.grad == p.l.x;
     const Val edge = tail && !f.zero ? K::val(x[rest]) : lowest(Val());
-    if (some) {
+    float own[2] = {};
+    bool mine[2] = {};
+    auto named_values = [&] {
+        uint64_t again[2];
+        named.repeated(here, again);
+        float add[2], sum[2] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) add[h] = lane_of(here[h]) ? part(h) : 0.f;
+        named.visit(here, [&](int j, int cls) {
+            const float aj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(j < 64 ? add[0] : add[1]), j & 63));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sum[h] += named.c[h] == cls ? aj : 0.f;
+        });
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            here[h] = here[h] && first[h] && tid < 64;
-            if (here[h]) own[h] = special(h, K::val(x[named.c[h]]), value);
+            mine[h] = lane_of(here[h] & ~again[h]);
+            if (mine[h]) own[h] = special(K::val(x[named.c[h]]), sum[h], value);
         }
+    };
+    if (some && over) {
+        if (tid < 64) named_values();
         __syncthreads();
     }
 #pragma unroll
@@ -688,10 +834,11 @@ __device__ __forceinline__ void store_gradient(const Params &p, uint64_t r, uint
     }
     if (tail) out[rest] = K::grad(f.zero ? 0.f : value(edge));
     if (some) {
+        if (!over && tid < 64) named_values();
         __syncthreads();
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (here[h]) out[named.c[h]] = K::grad(own[h]);
+            if (mine[h]) out[named.c[h]] = K::grad(own[h]);
     }
 }
 
@@ -717,28 +864,12 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(const LogprobsGr
     Named named;
     named.load(p.given + r * p.n_given, p.n_given);
     float u[2];
-    bool first[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const uint32_t c = (uint32_t)named.c[h];
         u[h] = named.c[h] < 0 ? 0.f : c < p.l.classes ? p.up_logprob[r * p.n_given + lane + 64 * h] : __builtin_nanf("");
     }
-    float up = u[0], sum[2] = {u[0], u[1]};
-    if (p.n_given == 1) {
-        up = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u[0]), 0));
-        first[0] = named.c[0] >= 0;
-        first[1] = false;
-    } else {
-        up = wave_sum(u[0] + u[1]);
-        sum[0] = sum[1] = 0.f;
-        first[0] = named.c[0] >= 0;
-        first[1] = named.c[1] >= 0;
-        named.pairs(p.n_given, [&](int h, uint32_t j, bool same) {
-            const float uj = __int_as_float(j < 64 ? __builtin_amdgcn_readlane(__float_as_int(u[0]), j) : __builtin_amdgcn_readlane(__float_as_int(u[1]), j - 64));
-            if (same) sum[h] += uj;
-            if (same && j < lane + 64 * h) first[h] = false;
-        });
-    }
+    const float up = p.n_given == 1 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u[0]), 0)) : wave_sum(u[0] + u[1]);
     const float uh = ENT ? p.up_entropy[r] : 0.f, logs = p.stats[2 * r + 1];
     Slope<Val> f;
     f.m = of_bits<Val>(p.stats[2 * r]);
@@ -746,7 +877,8 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(const LogprobsGr
     f.a0 = -p.l.scale * (up + (uh != 0.f ? uh * p.entropy[r] : 0.f));
     f.a1 = -p.l.scale * uh * LN2;
     f.zero = !(__any(named.c[0] >= 0 || named.c[1] >= 0) || uh != 0.f) || logs == NEG_INF;
-    store_gradient<TYPE, NV, ENT>(p, r, chunk, f, named, first, raw, [&](int h, Val v, auto value) { return value(v) + p.l.scale * sum[h]; });
+    store_gradient<TYPE, NV, ENT>(p, r, chunk, f, named, raw, [&](int h) { return u[h]; },
+                                  [&](Val v, float sum, auto value) { return value(v) + p.l.scale * sum; });
 }
 
 // w scale (Q p_j - sum of the q of j), and with the rest class for those that are no entry w scale (p_j / p_rest) (Q p_rest - q_rest)
@@ -775,21 +907,9 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillPara
         f.l2 = none ? 0.f : st.rest_logs * LOG2E;
         if (st.total != st.total) f.a0 = st.total;
     }
-    float q[2], sum[2] = {};
-    bool first[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        q[h] = named.c[h] >= 0 ? expf(p.value_scale * (teacher_value(p.value, p.value_type, r * p.top + lane + 64 * h) - st.value_m) - st.value_logs) : 0.f;
-        first[h] = named.c[h] >= 0;
-    }
-    named.pairs(p.top, [&](int h, uint32_t j, bool same) {
-        const float qj = __int_as_float(j < 64 ? __builtin_amdgcn_readlane(__float_as_int(q[0]), j) : __builtin_amdgcn_readlane(__float_as_int(q[1]), j - 64));
-        if (same) sum[h] += qj;
-        if (same && j < lane + 64 * h) first[h] = false;
-    });
-    store_gradient<TYPE, NV, false>(p, r, chunk, f, named, first, raw, [&](int h, Val v, auto) {
-        return p.l.scale * w * (st.total * __builtin_amdgcn_exp2f(c * below(v, m) - st.logs * LOG2E) - sum[h]);
-    });
+    store_gradient<TYPE, NV, false>(p, r, chunk, f, named, raw, [&](int h) {
+        return expf(p.value_scale * (teacher_value(p.value, p.value_type, r * p.top + lane + 64 * h) - st.value_m) - st.value_logs);
+    }, [&](Val v, float sum, auto) { return p.l.scale * w * (st.total * __builtin_amdgcn_exp2f(c * below(v, m) - st.logs * LOG2E) - sum); });
 }
 
 // ---- launches ------------------------------------------------------------------------
@@ -806,17 +926,19 @@ static void launch_chunks(const LogprobsParams &p, uint32_t rows, hipStream_t st
 template <int TYPE>
 static void launch_rows(const LogprobsParams &p, uint32_t nv, uint32_t rows, hipStream_t st) {
     if (nv == 2) launch_chunks<TYPE, 2>(p, rows, st);
+    else if (nv == 4) launch_chunks<TYPE, 4>(p, rows, st);
     else launch_chunks<TYPE, 8>(p, rows, st);
     if (p.chunks == 1) return;
-    if (p.top) hipLaunchKernelGGL((logprobs_join_kernel<TYPE, true>), dim3(rows), dim3(THREADS), 0, st, p);
-    else hipLaunchKernelGGL((logprobs_join_kernel<TYPE, false>), dim3(rows), dim3(THREADS), 0, st, p);
+    if (p.top && p.chunks <= 16 && p.list_cap <= 128) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, true>), dim3(rows), dim3(THREADS), 0, st, p);
+    else if (p.top) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, false>), dim3(rows), dim3(THREADS), 0, st, p);
+    else hipLaunchKernelGGL((logprobs_join_kernel<TYPE>), dim3(rows), dim3(64), 0, st, p);
 }
 
 RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top) {
     RowCut cut;
     const uint32_t per_vec = type == ISR_F32 || type == ISR_I32 ? 4 : 8, vecs = classes / per_vec;
     auto chunks_of = [&](uint32_t nv) { return vecs <= nv * THREADS ? 1 : (vecs + nv * THREADS - 1) / (nv * THREADS); };
-    cut.nv = rows * chunks_of(8) >= 1024 ? 8 : 2;
+    cut.nv = vecs <= 2 * THREADS ? 2 : vecs > 8 * THREADS && rows * chunks_of(8) <= 512 && chunks_of(4) <= 16 && top ? 4 : 8;
     cut.chunks = chunks_of(cut.nv);
     cut.chunk_vecs = vecs ? (vecs + cut.chunks - 1) / cut.chunks : 1;
     cut.list_cap = cut.chunks == 1 ? LIST : 2 * top + 64;
@@ -871,17 +993,7 @@ static void launch_distill_rows(const DistillParams &p, uint32_t nv, uint32_t ro
     else if (p.rest) hipLaunchKernelGGL((distill_kernel<TYPE, 8, true>), grid, block, 0, st, p);
     else if (nv == 2) hipLaunchKernelGGL((distill_kernel<TYPE, 2, false>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((distill_kernel<TYPE, 8, false>), grid, block, 0, st, p);
-    if (p.chunks > 1) hipLaunchKernelGGL((distill_join_kernel<TYPE>), dim3(rows), block, 0, st, p);
-}
-
-hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st) {
-    set_cut(p, cut);
-    p.parts = (Part *)workspace;
-    return by_runs(p, cut, [&](uint32_t rows) {
-#define CALL(T) launch_distill_rows<T>(p, cut.nv, rows, st)
-        BY_TYPE(p.l.type, CALL)
-#undef CALL
-    });
+    if (p.chunks > 1) hipLaunchKernelGGL((distill_join_kernel<TYPE>), dim3(rows), dim3(64), 0, st, p);
 }
 
 // Gradients keep less of a row in registers: nothing is exchanged between threads but the named classes.
@@ -909,14 +1021,30 @@ hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st) {
     });
 }
 
+static void launch_distill_grad_rows(const DistillParams &p, uint32_t rows, hipStream_t st) {
+#define CALL(T) hipLaunchKernelGGL((distill_grad_kernel<T, 4>), dim3(rows * p.chunks), dim3(THREADS), 0, st, p)
+    BY_TYPE(p.l.type, CALL)
+#undef CALL
+}
+
+hipError_t launch_distill(DistillParams p, RowCut cut, void *workspace, hipStream_t st) {
+    p.parts = (Part *)workspace;
+    const RowCut gradient = cut_gradient(p.l);
+    return by_runs(p, cut, [&](uint32_t rows) {
+        set_cut(p, cut);
+#define CALL(T) launch_distill_rows<T>(p, cut.nv, rows, st)
+        BY_TYPE(p.l.type, CALL)
+#undef CALL
+        if (!p.grad) return;
+        set_cut(p, gradient);
+        launch_distill_grad_rows(p, rows, st);
+    });
+}
+
 hipError_t launch_distill_grad(DistillParams p, hipStream_t st) {
     const RowCut cut = cut_gradient(p.l);
     set_cut(p, cut);
-    return by_runs(p, cut, [&](uint32_t rows) {
-#define CALL(T) hipLaunchKernelGGL((distill_grad_kernel<T, 4>), dim3(rows * p.chunks), dim3(THREADS), 0, st, p)
-        BY_TYPE(p.l.type, CALL)
-#undef CALL
-    });
+    return by_runs(p, cut, [&](uint32_t rows) { launch_distill_grad_rows(p, rows, st); });
 }
 
 }  // namespace isr
