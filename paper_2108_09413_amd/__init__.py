@@ -502,12 +502,16 @@ def _operand(t, shape, dtypes, x, what: str):
 
 
 def _on_device_of(x, call):
-    """Runs call(stream) with the logits' device current."""
+    """Runs call(current stream) with the logits' device current."""
     import torch
-    if x.device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream().cuda_stream)
-    with torch.cuda.device(x.device):
-        return call(torch.cuda.current_stream().cuda_stream)
+    index = x.device.index
+    # the stream's handle alone: a stream object around it costs as much as a launch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    stream = raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
+    if index == torch.cuda.current_device():
+        return call(stream)
+    with torch.cuda.device(index):
+        return call(stream)
 
 
 def _workspace(x, need: int):

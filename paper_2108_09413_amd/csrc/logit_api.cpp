@@ -9,7 +9,6 @@ namespace {
 using namespace isr;
 
 constexpr uint32_t MAX_CLASSES = 1u << 24;
-constexpr size_t DISTILL_STATS = 8 * sizeof(float);
 
 size_t element_bytes(int type) { return type == ISR_F32 || type == ISR_I32 ? 4 : 2; }
 bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -59,12 +58,12 @@ bool all_aligned(std::initializer_list<const void *> words) {
 
 LogitRows rows_of(const isr_logits *l) { return {l->data_device, l->type, l->classes, l->rows, l->row_stride, l->scale}; }
 
-DistillParams distill_params(const isr_logits *l, const isr_teacher *t, const float *weight, float *loss, float *stats, void *grad,
+DistillParams distill_params(const isr_logits *l, const isr_teacher *t, const float *weight, float *loss, const void *stats, void *grad,
                              uint64_t grad_stride) {
     DistillParams p{};
     p.l = rows_of(l);
     p.entry = t->class_device; p.value = t->logit_device; p.value_type = t->type; p.top = t->top; p.value_scale = t->scale; p.rest = t->rest;
-    p.weight = weight; p.loss = loss; p.stats = stats; p.grad = grad; p.grad_stride = grad_stride;
+    p.weight = weight; p.loss = loss; p.stats = (DistillStat *)stats; p.grad = grad; p.grad_stride = grad_stride;
     return p;
 }
 
@@ -80,7 +79,7 @@ extern "C" {
 
 size_t isr_logprobs_workspace_bytes(const isr_logits *l, uint32_t top) {
     if (!valid_shape(l) || l->rows == 0 || top > ISR_MAX_TOP) return 0;
-    const RowCut cut = cut_rows(l->type, l->classes, l->rows, top);
+    const RowCut cut = cut_logprobs(l->type, l->classes, l->rows, top);
     return cut.parts_bytes + cut.lists_bytes;
 }
 
@@ -93,7 +92,7 @@ int isr_logprobs(const isr_logits *l, const int32_t *given_device, uint32_t give
     if (given && (!given_device || !logprob_device)) return ISR_ERR_ARG;
     if (top && (!top_class_device || !top_logprob_device)) return ISR_ERR_ARG;
     if (!all_aligned({given_device, logprob_device, entropy_device, top_class_device, top_logprob_device, stats_device})) return ISR_ERR_ARG;
-    const RowCut cut = cut_rows(l->type, l->classes, l->rows, top);
+    const RowCut cut = cut_logprobs(l->type, l->classes, l->rows, top);
     const size_t need = cut.parts_bytes + cut.lists_bytes;
     if (need && (!workspace_device || workspace_bytes < need)) return ISR_ERR_WORKSPACE;
     if (need && !aligned(workspace_device, 16)) return ISR_ERR_ARG;
@@ -122,10 +121,10 @@ int isr_logprobs_grad(const isr_logits *l, const int32_t *given_device, uint32_t
     return status(launch_logprobs_grad(p, (hipStream_t)hip_stream));
 }
 
-// what the chunks of rows leave, and the rows' statistics when the caller keeps none: the gradient's kernel reads them
+// What the chunks of rows leave and, for a gradient behind them, the rows' statistics where the caller keeps none.
 size_t isr_distill_workspace_bytes(const isr_logits *l, const isr_teacher *t) {
     if (!valid_shape(l) || !valid_teacher(t) || l->rows == 0) return 0;
-    return cut_rows(l->type, l->classes, l->rows, 0).parts_bytes + l->rows * DISTILL_STATS;
+    return cut_distill(l->type, l->classes, l->rows, t->top).parts_bytes + (distill_in_one(l->type, l->classes, l->rows, t->top) ? 0 : l->rows * sizeof(DistillStat));
 }
 
 int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weight_device, float *loss_device, float *stats_device,
@@ -134,10 +133,12 @@ int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weig
     if (l->rows == 0) return ISR_OK;
     if (!teacher_data(t) || !loss_device || !all_aligned({row_weight_device, loss_device, stats_device})) return ISR_ERR_ARG;
     if (grad_logits_device && !valid_grad(l, grad_logits_device, grad_row_stride)) return ISR_ERR_ARG;
-    if (!workspace_device || workspace_bytes < isr_distill_workspace_bytes(l, t)) return ISR_ERR_WORKSPACE;
-    if (!aligned(workspace_device, 16)) return ISR_ERR_ARG;
-    const RowCut cut = cut_rows(l->type, l->classes, l->rows, 0);
-    float *stats = stats_device || !grad_logits_device ? stats_device : (float *)((uint8_t *)workspace_device + cut.parts_bytes);
+    const size_t need = isr_distill_workspace_bytes(l, t);
+    if (need && (!workspace_device || workspace_bytes < need)) return ISR_ERR_WORKSPACE;
+    if (need && !aligned(workspace_device, 16)) return ISR_ERR_ARG;
+    const RowCut cut = cut_distill(l->type, l->classes, l->rows, t->top);
+    void *stats = stats_device;
+    if (!stats && grad_logits_device && !distill_in_one(l->type, l->classes, l->rows, t->top)) stats = (uint8_t *)workspace_device + cut.parts_bytes;
     const DistillParams p = distill_params(l, t, row_weight_device, loss_device, stats, grad_logits_device, grad_row_stride);
     return status(launch_distill(p, cut, workspace_device, (hipStream_t)hip_stream));
 }
@@ -148,7 +149,7 @@ int isr_distill_grad(const isr_logits *l, const isr_teacher *t, const float *row
     if (l->rows == 0) return ISR_OK;
     if (!teacher_data(t) || !stats_device || !all_aligned({row_weight_device, stats_device})) return ISR_ERR_ARG;
     if (!valid_grad(l, grad_logits_device, grad_row_stride)) return ISR_ERR_ARG;
-    return status(launch_distill_grad(distill_params(l, t, row_weight_device, nullptr, const_cast<float *>(stats_device), grad_logits_device, grad_row_stride),
+    return status(launch_distill_grad(distill_params(l, t, row_weight_device, nullptr, stats_device, grad_logits_device, grad_row_stride),
                                       (hipStream_t)hip_stream));
 }
 

@@ -1,4 +1,4 @@
-// Operators on rows of class logits: what their entry points (logit_api.cpp) hand to their kernels (logit_rows.hip).
+// Operators on rows of class logits: what their entry points (logit_api.cpp) hand to their kernels (logprobs.hip, distill.hip).
 #pragma once
 #include "isr_internal.h"
 
@@ -12,18 +12,21 @@ struct LogitRows {
     float scale;
 };
 
-// How rows are cut into chunks of a workgroup each (cut_rows), and what the chunks need of the workspace.
+// How rows are cut into chunks of a workgroup each, and what the chunks need of the workspace.
 struct RowCut {
-    uint32_t nv;           // vectors of 16 bytes a thread
+    uint32_t nv;           // vectors of 16 bytes a thread; 0: 16 lanes a row
     uint32_t chunks;       // of a row
     uint32_t chunk_vecs;   // vectors of a chunk, the last one's may be fewer
     uint32_t list_cap;     // room for candidates of the top alternatives, of a chunk
     uint32_t rows;         // of a launch
     size_t parts_bytes, lists_bytes;
 };
-RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top);
+bool small_rows(uint32_t classes, uint32_t serial);
+RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, bool small);
+RowCut cut_gradient(const LogitRows &l, bool small);
 
 struct Part;
+// row0 to lists: set by the launcher, for each launch
 struct LogprobsParams {
     LogitRows l;
     const int32_t *given;
@@ -31,8 +34,8 @@ struct LogprobsParams {
     float *logprob, *entropy;
     int32_t *top_class;
     float *top_logprob, *stats;
-    // set by the launcher
     uint64_t row0;
+    uint32_t run;             // rows
     uint32_t chunks, chunk_vecs, list_cap;
     Part *parts;
     uint2 *lists;
@@ -45,10 +48,18 @@ struct LogprobsGradParams {
     const float *up_logprob, *entropy, *up_entropy, *stats;
     void *grad;
     uint64_t grad_stride;
-    // set by the launcher
     uint64_t row0;
-    uint32_t chunks, chunk_vecs;
+    uint32_t run, chunks, chunk_vecs;
 };
+
+// Statistics of a row between the loss and its gradient.  logs == -infinity: the gradient is zero.
+struct DistillStat {
+    float m, logs;               // of all classes; m: as the logits' type holds it
+    float rest_m, rest_logs;     // of those that are no entry (rest), else as m and logs
+    float value_m, value_logs;   // q = exp(value_scale (value - value_m) - value_logs)
+    float total, left;           // sum of q and q_rest; q_rest
+};
+static_assert(sizeof(DistillStat) == 32, "eight words a row");
 
 struct DistillParams {
     LogitRows l;
@@ -59,18 +70,23 @@ struct DistillParams {
     float value_scale;
     int32_t rest;
     const float *weight;
-    float *loss, *stats;      // stats: [rows][8], DistillStat
+    float *loss;
+    DistillStat *stats;
     void *grad;
     uint64_t grad_stride;
-    // set by the launcher
     uint64_t row0;
-    uint32_t chunks, chunk_vecs;
+    uint32_t run, chunks, chunk_vecs;
     Part *parts;
 };
 
+RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top);
 hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st);
 hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st);
-hipError_t launch_distill(DistillParams p, RowCut cut, void *workspace, hipStream_t st);   // and the gradient, if p.grad
+
+// Whether loss and gradient of rows of this shape are one launch, which needs neither a workspace nor the statistics.
+bool distill_in_one(int type, uint32_t classes, uint64_t rows, uint32_t top);
+RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top);
+hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st);   // the gradient too, if p.grad
 hipError_t launch_distill_grad(DistillParams p, hipStream_t st);
 
 }  // namespace isr
