@@ -185,8 +185,9 @@ size_t isr_noise_bank_static_capacity(void);
  * device memory, are enqueued on hip_stream (NULL = default; of the current device, which is the
  * one that holds the memory) and return at once: no allocation, no copy, no synchronisation, so
  * a call can be captured into a graph.  Workspaces (aligned to 16 bytes) hold nothing between calls; calls that may
- * overlap in time need a workspace each.  Results do not depend on the order in which workgroups
- * run.  Sums and statistics are fp32 or wider.
+ * overlap in time need a workspace each.  Sums and statistics are fp32 or wider.  Equal calls give
+ * equal bits; the last bits of a row's sums may depend on the number of rows and on whether the
+ * row starts at an even or an odd element.
  *
  * Logits x[r][j], j < classes, element (r, j) at data_device + r * row_stride + j (in elements);
  * aligned to their element, no more.  l = scale * x: scale is 1 / temperature, times the step of

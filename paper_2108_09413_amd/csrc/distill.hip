@@ -196,7 +196,7 @@ __device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(const Chunk
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>, WORDS = (NV + 3) / 4;
     const uint32_t tid = threadIdx.x;
-    bool tail = k.tail;
+    bool edge_valid = k.edge_valid;
     uint32_t out[WORDS] = {};   // bits of the entries among the thread's vectors, a byte each
     if constexpr (REST) {
 #pragma unroll
@@ -204,12 +204,14 @@ __device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(const Chunk
             if (i * T + tid < NV * T / 4) sh.bits[i * T + tid] = 0;
         if (tid == 0) sh.tail = 0;
         __syncthreads();
-        const uint32_t j = (uint32_t)entry - k.lo(), behind = (uint32_t)entry - (classes - classes % PV);
-        if (entry >= 0 && (uint32_t)entry >= k.lo() && j < k.n * PV) {
-            const uint32_t vec = j / PV, byte = vec % T * NV + vec / T;
-            atomicOr(&sh.bits[byte >> 2], 1u << (8 * (byte & 3) + j % PV));
-        } else if (entry >= 0 && (uint32_t)entry < classes && behind < PV) {
-            atomicOr(&sh.tail, 1u << behind);
+        if ((uint32_t)entry < classes && k.owns((uint32_t)entry)) {   // not negative either
+            const uint32_t j = (uint32_t)entry - k.first;
+            if (j < k.n * PV) {
+                const uint32_t vec = j / PV, byte = vec % T * NV + vec / T;
+                atomicOr(&sh.bits[byte >> 2], 1u << (8 * (byte & 3) + j % PV));
+            } else {
+                atomicOr(&sh.tail, 1u << ((uint32_t)entry < k.head ? PV - 1 : (uint32_t)entry - k.end));
+            }
         }
         __syncthreads();
         if constexpr (NV == 2) {
@@ -218,11 +220,11 @@ __device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(const Chunk
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) out[i] = sh.bits[tid * WORDS + i];
         }
-        tail = tail && !(sh.tail >> (tid & 31) & 1);
+        edge_valid = edge_valid && !(sh.tail >> (tid & 31) & 1);
     }
     auto bits = [&](int i) { return out[i / 4] >> (8 * (i & 3)) & 0xFF; };
     const Val edge = K::val(k.edge);
-    Stat<Val> a{tail ? edge : lowest(Val()), 0.f, 0.f};
+    Stat<Val> a{edge_valid ? edge : lowest(Val()), 0.f, 0.f};
     k.each([&](int i, uint32_t, Val (&v)[PV]) {
         if (REST && bits(i)) {
 #pragma unroll
@@ -232,7 +234,7 @@ __device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(const Chunk
         for (int e = 0; e < PV; ++e) a.m = larger(a.m, v[e]);
     });
     auto share = [&](Val v) { return __builtin_amdgcn_exp2f(c * below(v, a.m)); };
-    if (tail) a.s = share(edge);
+    if (edge_valid) a.s = share(edge);
     k.each([&](int i, uint32_t, const Val (&v)[PV]) {
         if (REST && bits(i)) {
 #pragma unroll

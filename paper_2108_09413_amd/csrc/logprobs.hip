@@ -41,26 +41,27 @@ template <> __device__ __forceinline__ uint32_t least_key<int32_t>() { return 0;
 template <class Val> constexpr int LOW_BITS = 16;                // fp32 keys: a relative step of 2^-7
 template <> constexpr int LOW_BITS<int32_t> = 0;
 
-// Every wave for itself: the largest bound of leading bits that k of the threads' keys reach, 0 if fewer threads have any.
-// Up to 32 alternatives the threads go by fours.
+// Every wave for itself: the largest bound of leading bits that k of the threads' keys reach, 0 if fewer threads have any.  Up to
+// 32 alternatives the threads go by fours, up to 64 by twos: fewer steps, and few more elements reach the bound.  The bits
+// that all keys share are not searched.
 template <int LOW>
 __device__ __forceinline__ uint32_t key_bound(const Shared &sh, uint32_t k) {
     const uint4 q = ((const uint4 *)sh.key)[threadIdx.x & 63];
-    uint32_t bound = 0;
-    if (k <= 32) {
-        const uint32_t top = max(max(q.x, q.y), max(q.z, q.w));
-        for (int b = 31; b >= LOW; --b) {
-            const uint32_t next = bound | (1u << b);
-            if ((uint32_t)__popcll(__ballot(top >= next)) >= k) bound = next;
-        }
-    } else {
-        for (int b = 31; b >= LOW; --b) {
-            const uint32_t next = bound | (1u << b);
-            const int n = __popcll(__ballot(q.x >= next)) + __popcll(__ballot(q.y >= next)) + __popcll(__ballot(q.z >= next)) + __popcll(__ballot(q.w >= next));
-            if ((uint32_t)n >= k) bound = next;
-        }
+    const uint32_t two[2] = {max(q.x, q.y), max(q.z, q.w)}, four = max(two[0], two[1]);
+    auto fold_min = [](uint32_t a, uint32_t b) { return min(a, b); };
+    auto fold_max = [](uint32_t a, uint32_t b) { return max(a, b); };
+    auto reach = [](uint32_t key, uint32_t next) { return (uint32_t)__popcll(__ballot(key >= next)); };
+    const uint32_t low = k <= 32 ? four : k <= 64 ? min(two[0], two[1]) : min(min(q.x, q.y), min(q.z, q.w));
+    const uint32_t least = wave_fold(low, fold_min), most = wave_fold(four, fold_max);
+    const int top = 31 - __builtin_clz((least ^ most) | 1);   // the highest bit in which two of them differ
+    uint32_t bound = (most >> top >> 1) << top << 1;
+    for (int b = top; b >= LOW; --b) {
+        const uint32_t next = bound | (1u << b);
+        const uint32_t n = k <= 32 ? reach(four, next) : k <= 64 ? reach(two[0], next) + reach(two[1], next)
+                                                                 : reach(q.x, next) + reach(q.y, next) + reach(q.z, next) + reach(q.w, next);
+        if (n >= k) bound = next;
     }
-    return bound;
+    return (bound >> LOW) << LOW;
 }
 
 __device__ __forceinline__ int block_count(int n, Shared &sh) {
@@ -172,31 +173,49 @@ __device__ __forceinline__ void finish_top(const LogprobsParams &p, uint64_t r, 
 }
 
 // A chunk of a row.
+constexpr int VECS = 256;
+template <bool TOP> struct SharedVecs {
+    uint4 raw[VECS];
+    uint32_t first[VECS], listed;
+};
+template <> struct SharedVecs<false> {};
 template <int TYPE, int NV, bool TOP, bool ENT>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams p) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>;
     __shared__ __attribute__((aligned(16))) Shared sh;
+    __shared__ __attribute__((aligned(16))) SharedVecs<TOP> vecs;
     const uint32_t tid = threadIdx.x, row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks;
     const uint64_t r = p.row0 + row;
-    const Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+    Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
     Given<TYPE> given;
     if (p.chunks == 1) given.load(p, r);
     const Val edge = K::val(k.edge);
-    Stat<Val> a{k.tail ? edge : lowest(Val()), 0.f, 0.f};
-    if (TOP && tid == 0) sh.listed = 0;
-    k.each([&](int, uint32_t, const Val (&v)[PV]) {
+    Stat<Val> a{k.edge_valid ? edge : lowest(Val()), 0.f, 0.f};
+    if constexpr (TOP) {
+        if (tid == 0) sh.listed = vecs.listed = 0;
+    }
+    Val most[NV];   // TOP: of each vector
+    k.each([&](int i, uint32_t, const Val (&v)[PV]) {
+        if constexpr (TOP) {
+            most[i] = v[0];
 #pragma unroll
-        for (int e = 0; e < PV; ++e) a.m = larger(a.m, v[e]);
+            for (int e = 1; e < PV; ++e) most[i] = larger(most[i], v[e]);
+            a.m = larger(a.m, most[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < PV; ++e) a.m = larger(a.m, v[e]);
+        }
     });
+    k.keep_packed();
     const float c = p.l.scale * LOG2E;
     auto add = [&](Val v) {
         const float d = c * below(v, a.m), e = __builtin_amdgcn_exp2f(d);
         a.s += e;
         if (ENT) a.t += e * fmaxf(d, NO_SHARE);
     };
-    if (k.tail) add(edge);
+    if (k.edge_valid) add(edge);
     k.each([&](int, uint32_t, const Val (&v)[PV]) {
 #pragma unroll
         for (int e = 0; e < PV; ++e) add(v[e]);
@@ -211,21 +230,31 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
                 if (at < LIST) sh.list[at] = make_uint2(key_of(v), ~cls);
             }
         };
-        if (a.m >= from) {
-            if (k.tail) take(edge, k.rest);
-            k.each([&](int, uint32_t j, const Val (&v)[PV]) {
-#pragma unroll
-                for (int e = 0; e < PV; ++e) take(v[e], j + e);
+        k.keep_packed();
+        // the few vectors that reach the bound, then their elements, a thread each
+        if (!(a.m < from)) {
+            if (k.edge_valid) take(edge, k.beside);
+            k.each([&](int i, uint32_t j, const Val (&)[PV]) {
+                if (!(most[i] < from)) {
+                    const uint32_t at = atomicAdd(&vecs.listed, 1u);
+                    if (at < VECS) { vecs.raw[at] = k.raw[i]; vecs.first[at] = j; }
+                }
             });
         }
+        __syncthreads();
+        const uint32_t n = vecs.listed;
+        for (uint32_t i = tid; i < min(n, (uint32_t)VECS) * PV; i += THREADS)
+            take(K::val(((const typename K::Raw *)vecs.raw)[i]), vecs.first[i / PV] + i % PV);
+        if (n > VECS && tid == 0) atomicMax(&sh.listed, LIST + 1u);   // some are missing: more than fit
         __syncthreads();
         if (sh.listed > p.list_cap) {   // uniform; from memory again, an element at a time
             __syncthreads();
             list_exactly([&](auto f) {
-                for (uint32_t j = k.lo() + tid; j < k.hi(p.l.classes); j += THREADS) {
+                for (uint32_t j = k.first + tid; j < k.first + k.n * PV; j += THREADS) {
                     const Val v = K::val(k.x[j]);
                     if (possible(v)) f(key_of(v), j);
                 }
+                if (k.edge_valid && possible(edge)) f(key_of(edge), k.beside);
             }, p.top, sh);
         }
     }
@@ -250,33 +279,35 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(const LogprobsParams 
     finish_values<TYPE>(p, p.row0 + blockIdx.x, all, given);
 }
 
-// FEW: at most 16 lists of at most 128: everything is read at once, the lists as far as they have room, and kept.
-template <int TYPE, bool FEW>
+// DEEP > 0: lists of at most 64 * DEEP, 8 / DEEP a wave at most: everything is read at once, the lists as far as they have room, and
+// kept.  One row of 131072 with 20 alternatives 10 -> 6 us.
+template <int TYPE, int DEEP>
 __global__ __launch_bounds__(THREADS) void logprobs_top_join_kernel(const LogprobsParams p) {
     using Val = typename Kind<TYPE>::Val;
+    constexpr int KEPT = 8;
     __shared__ __attribute__((aligned(16))) Shared sh;
     const uint32_t tid = threadIdx.x, row = blockIdx.x, lane = tid & 63, wave = tid >> 6;
     const Part *parts = p.parts + (size_t)row * p.chunks;
     const uint2 *lists = p.lists + (size_t)row * p.chunks * p.list_cap;
     Given<TYPE> given;
     given.load(p, p.row0 + row);
-    uint2 kept[FEW ? 8 : 1];
-    if constexpr (FEW) {
+    uint2 kept[KEPT];
+    if constexpr (DEEP != 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t q = wave + 4 * (i >> 1), at = lane + 64 * (i & 1);
+        for (int i = 0; i < KEPT; ++i) {
+            const uint32_t q = wave + 4 * (i / DEEP), at = lane + 64 * (i % DEEP);
             kept[i] = q < p.chunks && at < p.list_cap ? lists[(size_t)q * p.list_cap + at] : make_uint2(0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t q = wave + 4 * (i >> 1), at = lane + 64 * (i & 1);
-            if (q >= p.chunks || at >= parts[q].listed) kept[i] = make_uint2(0, 0);   // less than any key of a possible class
+        for (int i = 0; i < KEPT; ++i) {
+            const uint32_t q = wave + 4 * (i / DEEP), at = lane + 64 * (i % DEEP);
+            if (q >= p.chunks || at >= parts[q].listed) kept[i] = make_uint2(0, 0);   // ~class is never 0
         }
     }
     auto each = [&](auto f) {   // a wave a list
-        if constexpr (FEW) {
+        if constexpr (DEEP != 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < KEPT; ++i)
                 if (kept[i].y) f(kept[i].x, ~kept[i].y);
         } else {
             for (uint32_t q = wave; q < p.chunks; q += THREADS / 64) {
@@ -507,9 +538,12 @@ static void launch_rows(const LogprobsParams &p, uint32_t nv, hipStream_t st) {
     else if (nv == 4) launch_chunks<TYPE, 4>(p, st);
     else launch_chunks<TYPE, 8>(p, st);
     if (p.chunks == 1) return;
-    if (p.top && p.chunks <= 16 && p.list_cap <= 128) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, true>), dim3(p.run), dim3(THREADS), 0, st, p);
-    else if (p.top) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, false>), dim3(p.run), dim3(THREADS), 0, st, p);
-    else hipLaunchKernelGGL((logprobs_join_kernel<TYPE>), dim3(p.run), dim3(64), 0, st, p);
+    const dim3 grid(p.run), block(THREADS);
+    if (!p.top) hipLaunchKernelGGL((logprobs_join_kernel<TYPE>), grid, dim3(64), 0, st, p);
+    else if (p.chunks <= 16 && p.list_cap <= 128) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 2>), grid, block, 0, st, p);
+    else if (p.chunks <= 8 && p.list_cap <= 256) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 4>), grid, block, 0, st, p);
+    else if (p.chunks <= 4 && p.list_cap <= 512) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 8>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 0>), grid, block, 0, st, p);
 }
 
 RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top) { return cut_rows(type, classes, rows, top, small_rows(classes, top)); }
