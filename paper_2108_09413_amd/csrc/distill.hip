@@ -3,7 +3,8 @@
 // Loss alone: chunks of a row in registers, one workgroup each, and a join, as for the log-probabilities; with a rest class the
 // entries are left out of the chunks' sums.  Gradient alone: by elements from the row's statistics.
 // Both at once, rows that fit the registers of a workgroup (up to 16384 vectors of 16 bytes): the row is read once, held, and
-// its gradient stored from there.  Longer rows, and few, take the two ways one after the other.
+// its gradient stored from there, 4096 x 131072 bf16 with 64 entries and rest in 434 us (4.95 TB/s, of 5.8 that the
+// gradient alone reaches), 8192 x 32000 in 199 (5.3).  Longer rows take the two ways one after the other.
 // Rows of up to 256 classes go by 16 lanes each.
 #include <algorithm>
 
@@ -63,13 +64,15 @@ __device__ __forceinline__ void first_entries(const Named &e, uint32_t *table, b
         if (other[h]) is[h] = !lane_of(again[h]);
 }
 
-// What the teacher says, before anything is known of the student.  Sums over the entries that lead to q_rest are in 64 bits: it is
-// next to 0 where the entries hold nearly all.
+// What the teacher says, before anything is known of the student.  The sum that leads to q_rest is in 64 bits: it is next to 0
+// where the entries hold nearly all.  The same for all lanes but q and is.
 struct Taught {
-    double lq[2], q[2], total, left;   // log q, q, sum of q, q_rest
+    float q[2];
+    double total, left;   // sum of q and q_rest; q_rest
     float value_m, value_logs;
-    bool is[2];                        // first of its class
-    bool none, bad;                    // no teacher; no result
+    bool is[2];           // first of its class
+    bool none, bad;       // no teacher; no result
+    __device__ __forceinline__ double logq(const DistillParams &p, float v) const { return (double)p.value_scale * ((double)v - value_m) - value_logs; }
 };
 template <int TYPE>
 __device__ __forceinline__ Taught taught(const DistillParams &p, const Entries<TYPE> &e, uint32_t *table) {
@@ -80,29 +83,30 @@ __device__ __forceinline__ Taught taught(const DistillParams &p, const Entries<T
     t.bad = __any(bad);
     t.value_m = p.rest ? 0.f : wave_max(larger(e.v[0], e.v[1]));
     t.none = !__any(e.c[0] >= 0 || e.c[1] >= 0) || t.value_m == NEG_INF;
+    if (t.none) t.value_m = 0.f;
     t.value_logs = 0.f;
     t.left = 0.0;
     first_entries(e, table, t.is);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) t.lq[h] = (double)p.value_scale * ((double)e.v[h] - (t.none ? 0.f : t.value_m));
     if (p.rest) {
+        double sum = 0.0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) t.q[h] = e.c[h] >= 0 ? exp(t.lq[h]) : 0.0;
-        t.total = wave_sum(t.q[0] + t.q[1]);
-        t.left = fmax(1.0 - t.total, 0.0);
+        for (int h = 0; h < 2; ++h) {
+            const double q = e.c[h] >= 0 ? exp(t.logq(p, e.v[h])) : 0.0;
+            sum += q;
+            t.q[h] = (float)q;
+        }
+        sum = wave_sum(sum);
+        t.left = fmax(1.0 - sum, 0.0);
+        t.total = sum + t.left;
     } else {
         float z = 0.f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) z += e.c[h] >= 0 ? expf((float)t.lq[h]) : 0.f;
+        for (int h = 0; h < 2; ++h) z += e.c[h] >= 0 ? expf((float)t.logq(p, e.v[h])) : 0.f;
         t.value_logs = logf(wave_sum(z));
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            t.lq[h] -= t.value_logs;
-            t.q[h] = e.c[h] >= 0 ? expf((float)t.lq[h]) : 0.f;
-        }
-        t.total = wave_sum(t.q[0] + t.q[1]);
+        for (int h = 0; h < 2; ++h) t.q[h] = e.c[h] >= 0 ? expf((float)t.logq(p, e.v[h])) : 0.f;
+        t.total = wave_sum((double)t.q[0] + t.q[1]);
     }
-    t.total += t.left;
     return t;
 }
 
@@ -136,7 +140,7 @@ __device__ __forceinline__ DistillStat conclude(const DistillParams &p, uint64_t
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const double lp = empty || !possible(e.at[h]) ? (double)NEG_INF : (double)p.l.scale * below64(e.at[h], all.m) - logs;
-        if (t.q[h] > 0.0) loss += t.q[h] * (t.lq[h] - lp);
+        if (t.q[h] > 0.f) loss += (double)t.q[h] * (t.logq(p, e.v[h]) - lp);
     }
     loss = wave_sum(loss);
     if (t.left > 0.0) {
@@ -191,7 +195,7 @@ template <bool REST, int T, int NV> struct SharedMask { uint32_t bits[NV * T / 4
 template <int T, int NV> struct SharedMask<false, T, NV> {};
 
 template <bool REST, int TYPE, int T, int NV>
-__device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(const Chunk<TYPE, T, NV> &k, uint32_t classes, float c, int32_t entry, SharedMask<REST, T, NV> &sh) {
+__device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(Chunk<TYPE, T, NV> &k, uint32_t classes, float c, int32_t entry, SharedMask<REST, T, NV> &sh) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>, WORDS = (NV + 3) / 4;
@@ -233,6 +237,7 @@ __device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(const Chunk
 #pragma unroll
         for (int e = 0; e < PV; ++e) a.m = larger(a.m, v[e]);
     });
+    k.keep_packed();
     auto share = [&](Val v) { return __builtin_amdgcn_exp2f(c * below(v, a.m)); };
     if (edge_valid) a.s = share(edge);
     k.each([&](int i, uint32_t, const Val (&v)[PV]) {
@@ -258,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p)
     const uint64_t r = p.row0 + row;
     // in front of the row's loads, behind which it would have to wait for them
     const int32_t entry = REST && tid < p.top ? p.entry[r * p.top + tid] : -1;
-    const Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+    Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
     const float c = p.l.scale * LOG2E;
     const Stat<Val> all = block_stat<THREADS, false>(chunk_stat<REST>(k, p.l.classes, c, entry, mask), c, sh, [] {});
     if (p.chunks > 1) {
@@ -299,7 +304,7 @@ __global__ __launch_bounds__(T) void distill_row_kernel(const DistillParams p) {
     Entries<TYPE> e;
     if (tid < 64) e.load(p, r);
     const float w = p.weight ? p.weight[r] : 1.f;
-    const Chunk<TYPE, T, NV> k(p.l, r, 0, 1, p.chunk_vecs);
+    Chunk<TYPE, T, NV> k(p.l, r, 0, 1, p.chunk_vecs);
     Taught t;
     if (tid < 64) t = taught<TYPE>(p, e, table);   // while the row arrives
     const float c = p.l.scale * LOG2E;
@@ -318,10 +323,9 @@ __global__ __launch_bounds__(T) void distill_row_kernel(const DistillParams p) {
     store_slopes(k, out, f);
     __syncthreads();
     if (tid >= 64 || f.zero) return;
-    const float q[2] = {(float)t.q[0], (float)t.q[1]};
-    float sum[2] = {q[0], q[1]};
+    float sum[2] = {t.q[0], t.q[1]};
     const uint64_t again[2] = {__ballot(e.c[0] >= 0 && !t.is[0]), __ballot(e.c[1] >= 0 && !t.is[1])};
-    e.add_same(again, q, sum);
+    e.add_same(again, t.q, sum);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
         if (t.is[h] && (uint32_t)e.c[h] < p.l.classes) out[e.c[h]] = K::grad(entry_slope(p, st, w, e.at[h], sum[h]));
@@ -480,11 +484,7 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
 static uint32_t vecs_of(int type, uint32_t classes) { return classes / (type == ISR_F32 || type == ISR_I32 ? 4 : 8); }
 static bool small(uint32_t classes, uint32_t top) { return small_rows(classes, top); }
 
-bool distill_in_one(int type, uint32_t classes, uint64_t rows, uint32_t top) {
-    if (small(classes, top)) return true;
-    const uint32_t vecs = vecs_of(type, classes);
-    return vecs <= 8 * THREADS || (vecs <= 16 * 1024 && rows >= 128);
-}
+bool distill_in_one(int type, uint32_t classes, uint32_t top) { return small(classes, top) || vecs_of(type, classes) <= 16 * 1024; }
 
 RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top) { return cut_rows(type, classes, rows, 0, small(classes, top)); }
 
@@ -512,6 +512,8 @@ static void launch_loss(const DistillParams &p, uint32_t nv, hipStream_t st) {
     if (p.chunks > 1) hipLaunchKernelGGL((distill_join_kernel<TYPE>), dim3(p.run), dim3(64), 0, st, p);
 }
 
+// 16 vectors a thread and as few threads as that takes: several workgroups share a CU, and what one sums another's loads cover.  us with
+// 256 threads of 16 / 1024 of 8: 8192 x 24000 bf16 148 / 231, 8192 x 32000 199 / 263, with 512 of 16: 4096 x 64000 195 / 227.
 template <int TYPE>
 static void launch_in_one(DistillParams &p, hipStream_t st) {
     const uint32_t vecs = vecs_of(TYPE, p.l.classes);
@@ -519,7 +521,8 @@ static void launch_in_one(DistillParams &p, hipStream_t st) {
     p.chunk_vecs = vecs;
     if (vecs <= 2 * THREADS) launch_row_kernel<TYPE, THREADS, 2>(p, st);
     else if (vecs <= 8 * THREADS) launch_row_kernel<TYPE, THREADS, 8>(p, st);
-    else if (vecs <= 8 * 1024) launch_row_kernel<TYPE, 1024, 8>(p, st);
+    else if (vecs <= 16 * THREADS) launch_row_kernel<TYPE, THREADS, 16>(p, st);
+    else if (vecs <= 16 * 512) launch_row_kernel<TYPE, 512, 16>(p, st);
     else launch_row_kernel<TYPE, 1024, 16>(p, st);
 }
 
@@ -530,7 +533,7 @@ static void launch_gradient(const DistillParams &p, uint32_t nv, hipStream_t st)
 }
 
 hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st) {
-    const bool in_one = p.grad && distill_in_one(p.l.type, p.l.classes, p.l.rows, p.top);
+    const bool in_one = p.grad && distill_in_one(p.l.type, p.l.classes, p.top);
     const RowCut gradient = cut_gradient(p.l, cut.nv == 0);
     p.parts = (Part *)workspace;
     return by_runs(p, cut.rows, [&](uint32_t rows) {

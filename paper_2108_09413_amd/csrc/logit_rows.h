@@ -84,7 +84,7 @@ hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace,
 hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st);
 
 // Whether loss and gradient of rows of this shape are one launch, which needs neither a workspace nor the statistics.
-bool distill_in_one(int type, uint32_t classes, uint64_t rows, uint32_t top);
+bool distill_in_one(int type, uint32_t classes, uint32_t top);
 RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top);
 hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st);   // the gradient too, if p.grad
 hipError_t launch_distill_grad(DistillParams p, hipStream_t st);
