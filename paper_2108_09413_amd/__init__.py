@@ -471,9 +471,15 @@ class Distilled(NamedTuple):
     grad: object       # [rows, classes] of the logits' type
 
 
+_torch_types = {}
+
+
 def _types():
-    import torch
-    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32}
+    """Element type of each torch type, filled when torch is there."""
+    if not _torch_types:
+        import torch
+        _torch_types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32})
+    return _torch_types
 
 
 def _refuse(why: str):
@@ -501,22 +507,26 @@ def _operand(t, shape, dtypes, x, what: str):
     return t.data_ptr()
 
 
-def _on_device_of(x, call):
-    """Runs call(current stream) with the logits' device current."""
+def _on_device_of(x, entry, *args):
+    """Calls entry(*args, current stream) of the library with the logits' device current."""
     import torch
-    index = x.device.index
+    index = x.get_device()
     # the stream's handle alone: a stream object around it costs as much as a launch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     stream = raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
     if index == torch.cuda.current_device():
-        return call(stream)
+        return entry(*args, stream)
     with torch.cuda.device(index):
-        return call(stream)
+        return entry(*args, stream)
 
 
 def _workspace(x, need: int):
+    """Memory and its address; none for 0 bytes."""
+    if not need:
+        return None, None
     import torch
-    return torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    ws = x.new_empty(need, dtype=torch.uint8)
+    return ws, ws.data_ptr()
 
 
 def _grad_rows(x, out):
@@ -524,7 +534,7 @@ def _grad_rows(x, out):
     import torch
     dtype = torch.float32 if x.dtype == torch.int32 else x.dtype
     if out is None:
-        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+        out = x.new_empty(x.shape, dtype=dtype)
     elif out.dtype != dtype or out.shape != x.shape or out.device != x.device or (x.shape[1] > 1 and x.shape[0] and out.stride(1) != 1):
         _refuse(f"gradient {out.dtype} {tuple(out.shape)} of logits {x.dtype} {tuple(x.shape)}")
     return out, out.stride(0) if x.shape[0] > 1 else x.shape[1]
@@ -535,23 +545,22 @@ def isr_logprobs(logits, given=None, top: int = 0, entropy: bool = False, scale:
     of rows of logits, on the current stream of their device."""
     import torch
     l = _logits(logits, scale)
-    rows, f32 = l.rows, torch.float32
-    n = 0
+    rows, n, f32 = logits.shape[0], 0, torch.float32
     if given is not None:
         if given.dim() != 2:
             _refuse("given classes are [rows, given]")
         n = given.shape[1]
     pg = _operand(given, (rows, n), (torch.int32,), logits, "given classes")
-
-    def new(*shape, dtype=f32):
-        return torch.empty(shape, dtype=dtype, device=logits.device)
-    r = LogProbs(new(rows, n) if n else None, new(rows) if entropy else None, new(rows, top, dtype=torch.int32) if top > 0 else None,
-                 new(rows, top) if top > 0 else None, new(rows, 2) if stats else None)
-    need = lib().isr_logprobs_workspace_bytes(C.byref(l), max(top, 0))
-    ws = _workspace(logits, need)
+    if top < 0:
+        _refuse(f"top = {top}")
+    new = logits.new_empty
+    r = LogProbs(new((rows, n), dtype=f32) if n else None, new(rows, dtype=f32) if entropy else None,
+                 new((rows, top), dtype=torch.int32) if top else None, new((rows, top), dtype=f32) if top else None,
+                 new((rows, 2), dtype=f32) if stats else None)
+    need = lib().isr_logprobs_workspace_bytes(l, top)
+    ws, pw = _workspace(logits, need)
     p = [t.data_ptr() if t is not None else None for t in r]
-    _check(_on_device_of(logits, lambda st: lib().isr_logprobs(C.byref(l), pg, n, top if top >= 0 else ~0 & 0xFFFFFFFF, *p,
-                                                               ws.data_ptr() if need else None, need, st)), "isr_logprobs")
+    _check(_on_device_of(logits, lib().isr_logprobs, l, pg, n, top, *p, pw, need), "isr_logprobs")
     return r
 
 
@@ -571,7 +580,7 @@ def isr_logprobs_grad(logits, given, grad_logprob, stats, entropy=None, grad_ent
          _operand(entropy, (l.rows,), f32, logits, "entropy"), _operand(grad_entropy, (l.rows,), f32, logits, "gradient of the entropy"),
          _operand(stats, (l.rows, 2), f32, logits, "statistics")]
     out, stride = _grad_rows(logits, out)
-    _check(_on_device_of(logits, lambda st: lib().isr_logprobs_grad(C.byref(l), *p, out.data_ptr(), stride, st)), "isr_logprobs_grad")
+    _check(_on_device_of(logits, lib().isr_logprobs_grad, l, *p, out.data_ptr(), stride), "isr_logprobs_grad")
     return out
 
 
@@ -593,14 +602,13 @@ def isr_distill(logits, teacher_class, teacher_logit, weight=None, rest: bool = 
     l = _logits(logits, scale)
     t = _teacher(logits, l, teacher_class, teacher_logit, teacher_scale, rest)
     pw = _operand(weight, (l.rows,), (torch.float32,), logits, "weights")
-    loss = torch.empty(l.rows, dtype=torch.float32, device=logits.device)
-    st8 = torch.empty((l.rows, 8), dtype=torch.float32, device=logits.device) if stats else None
+    loss = logits.new_empty(l.rows, dtype=torch.float32)
+    st8 = logits.new_empty((l.rows, 8), dtype=torch.float32) if stats else None
     out, stride = (None, 0) if grad is None or grad is False else _grad_rows(logits, None if grad is True else grad)
-    need = lib().isr_distill_workspace_bytes(C.byref(l), C.byref(t))
-    ws = _workspace(logits, need)
-    _check(_on_device_of(logits, lambda st: lib().isr_distill(C.byref(l), C.byref(t), pw, loss.data_ptr(), st8.data_ptr() if stats else None,
-                                                              out.data_ptr() if out is not None else None, stride,
-                                                              ws.data_ptr() if need else None, need, st)), "isr_distill")
+    need = lib().isr_distill_workspace_bytes(l, t)
+    ws, pws = _workspace(logits, need)
+    _check(_on_device_of(logits, lib().isr_distill, l, t, pw, loss.data_ptr(), st8.data_ptr() if stats else None,
+                         out.data_ptr() if out is not None else None, stride, pws, need), "isr_distill")
     return Distilled(loss, st8, out)
 
 
@@ -613,8 +621,7 @@ def isr_distill_grad(logits, teacher_class, teacher_logit, stats, weight=None, r
     f32 = (torch.float32,)
     pw, ps = _operand(weight, (l.rows,), f32, logits, "weights"), _operand(stats, (l.rows, 8), f32, logits, "statistics")
     out, stride = _grad_rows(logits, out)
-    _check(_on_device_of(logits, lambda st: lib().isr_distill_grad(C.byref(l), C.byref(t), pw, ps, out.data_ptr(), stride, st)),
-           "isr_distill_grad")
+    _check(_on_device_of(logits, lib().isr_distill_grad, l, t, pw, ps, out.data_ptr(), stride), "isr_distill_grad")
     return out
 
 
