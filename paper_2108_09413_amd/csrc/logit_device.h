@@ -201,6 +201,8 @@ struct Chunk {
         edge = x[last ? min(beside, l.classes - 1) : head];   // of use where edge_valid
     }
     __device__ __forceinline__ bool owns(uint32_t j) const { return j - first < n * PV || (last && (j < head || j >= end)); }   // j below the number of classes
+    __device__ __forceinline__ bool has(int i) const { return i * T + threadIdx.x < n; }
+    __device__ __forceinline__ uint32_t at(int i) const { return first + (i * T + threadIdx.x) * PV; }
     // Between two passes over the vectors: what one has unpacked is not held in registers for the next.
     __device__ __forceinline__ void keep_packed() {
 #pragma unroll
@@ -211,10 +213,10 @@ struct Chunk {
     __device__ __forceinline__ void each(F f) const {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (i * T + threadIdx.x >= n) continue;
+            if (!has(i)) continue;
             Val v[PV];
             unpack<TYPE>(raw[i], v);
-            f(i, first + (i * T + threadIdx.x) * PV, v);
+            f(i, at(i), v);
         }
     }
 };

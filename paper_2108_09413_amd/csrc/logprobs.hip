@@ -38,12 +38,11 @@ template <> __device__ __forceinline__ int32_t of_key<int32_t>(uint32_t k) { ret
 template <class Val> __device__ __forceinline__ uint32_t least_key();   // of a possible class
 template <> __device__ __forceinline__ uint32_t least_key<float>() { return 0x00800000u; }
 template <> __device__ __forceinline__ uint32_t least_key<int32_t>() { return 0; }
-template <class Val> constexpr int LOW_BITS = 16;                // fp32 keys: a relative step of 2^-7
-template <> constexpr int LOW_BITS<int32_t> = 0;
+template <int TYPE> constexpr int LOW_BITS = TYPE == ISR_BF16 ? 16 : TYPE == ISR_F16 ? 13 : 0;   // of a key, the same in all of them
 
 // Every wave for itself: the largest bound of leading bits that k of the threads' keys reach, 0 if fewer threads have any.  Up to
-// 32 alternatives the threads go by fours, up to 64 by twos: fewer steps, and few more elements reach the bound.  The bits
-// that all keys share are not searched.
+// 32 alternatives the threads go by fours, up to 64 by twos: fewer steps, and few more elements reach the bound.  From the first
+// bit in which keys differ; below 16 bits only where that leaves many.
 template <int LOW>
 __device__ __forceinline__ uint32_t key_bound(const Shared &sh, uint32_t k) {
     const uint4 q = ((const uint4 *)sh.key)[threadIdx.x & 63];
@@ -54,13 +53,17 @@ __device__ __forceinline__ uint32_t key_bound(const Shared &sh, uint32_t k) {
     const uint32_t low = k <= 32 ? four : k <= 64 ? min(two[0], two[1]) : min(min(q.x, q.y), min(q.z, q.w));
     const uint32_t least = wave_fold(low, fold_min), most = wave_fold(four, fold_max);
     const int top = 31 - __builtin_clz((least ^ most) | 1);   // the highest bit in which two of them differ
-    uint32_t bound = (most >> top >> 1) << top << 1;
-    for (int b = top; b >= LOW; --b) {
-        const uint32_t next = bound | (1u << b);
-        const uint32_t n = k <= 32 ? reach(four, next) : k <= 64 ? reach(two[0], next) + reach(two[1], next)
-                                                                 : reach(q.x, next) + reach(q.y, next) + reach(q.z, next) + reach(q.w, next);
-        if (n >= k) bound = next;
-    }
+    uint32_t bound = (most >> top >> 1) << top << 1, reached = THREADS;
+    auto search = [&](int from, int to) {
+        for (int b = from; b >= to; --b) {
+            const uint32_t next = bound | (1u << b);
+            const uint32_t n = k <= 32 ? reach(four, next) : k <= 64 ? reach(two[0], next) + reach(two[1], next)
+                                                                     : reach(q.x, next) + reach(q.y, next) + reach(q.z, next) + reach(q.w, next);
+            if (n >= k) { bound = next; reached = n; }
+        }
+    };
+    search(top, max(LOW, 16));
+    if (LOW < 16 && reached > 2 * k + 16) search(min(top, 15), LOW);   // logits closer to each other than 2^-7 of their size
     return (bound >> LOW) << LOW;
 }
 
@@ -74,30 +77,24 @@ __device__ __forceinline__ int block_count(int n, Shared &sh) {
 }
 
 // each(f): f(key, class) for the thread's own possible elements, of which all threads together have more than k.  Lists
-// exactly k.  Returns with the list complete for all threads.
+// exactly k: the bound is a number of 56 bits, key and ~class (below 2^24), found bit by bit.  Returns with the list complete for
+// all threads.  Rows of equal logits come here, 2048 x 65536 bf16 with 20 alternatives 2.0 ms where other rows take 0.06.
 template <class Each>
 __device__ void list_exactly(Each each, uint32_t k, Shared &sh) {
-    uint32_t hi = 0, lo = 0;
-    bool done = false;
-    for (int b = 31; b >= 0 && !done; --b) {
-        const uint32_t next = hi | (1u << b);
+    uint64_t bound = 0;
+    auto number = [](uint32_t key, uint32_t cls) { return (uint64_t)key << 24 | (~cls & 0xFFFFFF); };
+    for (int b = 55; b >= 0; --b) {
+        const uint64_t next = bound | (1ull << b);
         int n = 0;
-        each([&](uint32_t key, uint32_t) { n += key >= next; });
+        each([&](uint32_t key, uint32_t cls) { n += number(key, cls) >= next; });
         n = block_count(n, sh);
-        if ((uint32_t)n >= k) { hi = next; done = (uint32_t)n == k; }
-    }
-    if (!done) lo = 0xFF000000u;   // classes are below 2^24
-    for (int b = 23; b >= 0 && !done; --b) {
-        const uint32_t next = lo | (1u << b);
-        int n = 0;
-        each([&](uint32_t key, uint32_t cls) { n += key > hi || (key == hi && ~cls >= next); });
-        n = block_count(n, sh);
-        if ((uint32_t)n >= k) { lo = next; done = (uint32_t)n == k; }
+        if ((uint32_t)n >= k) bound = next;
+        if ((uint32_t)n == k) break;
     }
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
     each([&](uint32_t key, uint32_t cls) {
-        if (key > hi || (key == hi && ~cls >= lo)) {
+        if (number(key, cls) >= bound) {
             const uint32_t at = atomicAdd(&sh.listed, 1u);
             if (at < LIST) sh.list[at] = make_uint2(key, ~cls);
         }
@@ -172,20 +169,72 @@ __device__ __forceinline__ void finish_top(const LogprobsParams &p, uint64_t r, 
     }
 }
 
-// A chunk of a row.
-constexpr int VECS = 256;
-template <bool TOP> struct SharedVecs {
+// Places in a list for the lanes that want one, by one atomic a wave: an atomic a candidate, each waited for, took longer than
+// anything else behind the loads (top 64 of 2048 x 32771 f32, 65 -> 58 us).
+__device__ __forceinline__ uint32_t places(uint32_t n, uint32_t *listed) {   // of n, the same in the wave
+    uint32_t base = 0;
+    if ((threadIdx.x & 63) == 0) base = atomicAdd(listed, n);
+    return __builtin_amdgcn_readfirstlane(base);
+}
+__device__ __forceinline__ uint32_t lanes_before(uint64_t of) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(of >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)of, 0)); }
+
+// The elements that reach the bound, of those that the wave's lanes have; by all its lanes.
+template <class Val>
+__device__ __forceinline__ void list_element(bool valid, Val v, uint32_t cls, Val from, Shared &sh) {
+    const uint64_t of = __ballot(valid && v >= from);
+    if (!of) return;
+    const uint32_t at = places(__popcll(of), &sh.listed) + lanes_before(of);
+    if (lane_of(of) && at < LIST) sh.list[at] = make_uint2(key_of(v), ~cls);
+}
+
+// Vectors that hold candidates, with their first class.
+constexpr int VECS = 512;
+struct SharedVecs {
     uint4 raw[VECS];
     uint32_t first[VECS], listed;
 };
-template <> struct SharedVecs<false> {};
+struct Nothing {};
+
+// The chunk's vectors that reach the bound (few; NaN does, all results of its row are NaN).
+template <int TYPE, int NV>
+__device__ __forceinline__ void list_vectors(const Chunk<TYPE, THREADS, NV> &k, const typename Kind<TYPE>::Val (&most)[NV], typename Kind<TYPE>::Val from, SharedVecs &vecs) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) n += __popcll(__ballot(k.has(i) && !(most[i] < from)));
+    if (n == 0) return;
+    uint32_t at = places(n, &vecs.listed);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint64_t of = __ballot(k.has(i) && !(most[i] < from));
+        const uint32_t mine = at + lanes_before(of);
+        if (lane_of(of) && mine < VECS) {
+            vecs.raw[mine] = k.raw[i];
+            vecs.first[mine] = k.at(i);
+        }
+        at += __popcll(of);
+    }
+}
+
+// Their elements to the list, a thread each.  Between two barriers of the caller.
+template <int TYPE>
+__device__ __forceinline__ void list_elements(const SharedVecs &vecs, typename Kind<TYPE>::Val from, Shared &sh) {
+    using K = Kind<TYPE>;
+    constexpr int PV = PER_VEC<TYPE>;
+    const uint32_t n = min(vecs.listed, (uint32_t)VECS) * PV;
+    for (uint32_t i0 = 0; i0 < n; i0 += THREADS) {
+        const uint32_t i = i0 + threadIdx.x, j = min(i, n - 1);
+        list_element(i < n, K::val(((const typename K::Raw *)vecs.raw)[j]), vecs.first[j / PV] + j % PV, from, sh);
+    }
+}
+
+// A chunk of a row.
 template <int TYPE, int NV, bool TOP, bool ENT>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams p) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>;
     __shared__ __attribute__((aligned(16))) Shared sh;
-    __shared__ __attribute__((aligned(16))) SharedVecs<TOP> vecs;
+    __shared__ __attribute__((aligned(16))) std::conditional_t<TOP, SharedVecs, Nothing> vecs;
     const uint32_t tid = threadIdx.x, row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks;
     const uint64_t r = p.row0 + row;
     Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
@@ -222,37 +271,34 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
     });
     const Stat<Val> all = block_stat<THREADS, ENT>(a, c, sh, [&] { if (TOP) sh.key[tid] = key_of(a.m); });
     if constexpr (TOP) {
-        const uint32_t bound = key_bound<LOW_BITS<Val>>(sh, p.top);
+        const uint32_t bound = key_bound<LOW_BITS<TYPE>>(sh, p.top);
         const Val from = of_key<Val>(max(bound, least_key<Val>()));
-        auto take = [&](Val v, uint32_t cls) {
-            if (v >= from) {
-                const uint32_t at = atomicAdd(&sh.listed, 1u);
-                if (at < LIST) sh.list[at] = make_uint2(key_of(v), ~cls);
-            }
-        };
         k.keep_packed();
-        // the few vectors that reach the bound, then their elements, a thread each
-        if (!(a.m < from)) {
-            if (k.edge_valid) take(edge, k.beside);
-            k.each([&](int i, uint32_t j, const Val (&)[PV]) {
-                if (!(most[i] < from)) {
-                    const uint32_t at = atomicAdd(&vecs.listed, 1u);
-                    if (at < VECS) { vecs.raw[at] = k.raw[i]; vecs.first[at] = j; }
-                }
-            });
-        }
+        // the few vectors that reach the bound, then their elements
+        if (p.chunks == 1 || chunk == p.chunks - 1) list_element(k.edge_valid, edge, k.beside, from, sh);
+        list_vectors(k, most, from, vecs);
         __syncthreads();
-        const uint32_t n = vecs.listed;
-        for (uint32_t i = tid; i < min(n, (uint32_t)VECS) * PV; i += THREADS)
-            take(K::val(((const typename K::Raw *)vecs.raw)[i]), vecs.first[i / PV] + i % PV);
-        if (n > VECS && tid == 0) atomicMax(&sh.listed, LIST + 1u);   // some are missing: more than fit
+        list_elements<TYPE>(vecs, from, sh);
+        if (vecs.listed > VECS && tid == 0) atomicMax(&sh.listed, LIST + 1u);   // some are missing: more than fit
         __syncthreads();
-        if (sh.listed > p.list_cap) {   // uniform; from memory again, an element at a time
+        const uint32_t listed = sh.listed;   // uniform
+        if (listed > p.list_cap && listed <= LIST) {   // neighbours that reach the bound together: of the listed, two a thread
+            const uint2 mine[2] = {tid < listed ? sh.list[tid] : make_uint2(0, 0), tid + THREADS < listed ? sh.list[tid + THREADS] : make_uint2(0, 0)};
             __syncthreads();
             list_exactly([&](auto f) {
-                for (uint32_t j = k.first + tid; j < k.first + k.n * PV; j += THREADS) {
-                    const Val v = K::val(k.x[j]);
-                    if (possible(v)) f(key_of(v), j);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (mine[h].y) f(mine[h].x, ~mine[h].y);   // ~class is never 0
+            }, p.top, sh);
+        } else if (listed > LIST) {   // from memory again
+            __syncthreads();
+            list_exactly([&](auto f) {
+                for (uint32_t j = k.first + tid * PV; j < k.first + k.n * PV; j += THREADS * PV) {
+                    Val v[PV];
+                    unpack<TYPE>(((const Loose *)(k.x + j))->v, v);
+#pragma unroll
+                    for (int e = 0; e < PV; ++e)
+                        if (possible(v[e])) f(key_of(v[e]), j + e);
                 }
                 if (k.edge_valid && possible(edge)) f(key_of(edge), k.beside);
             }, p.top, sh);
@@ -325,7 +371,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_top_join_kernel(const Logpro
     if (tid == 0) sh.listed = 0;
     const Stat<Val> all = join_parts<Val>(parts, p.chunks, p.l.scale * LOG2E);   // every wave for itself
     __syncthreads();
-    const uint32_t bound = key_bound<LOW_BITS<Val>>(sh, p.top);
+    const uint32_t bound = key_bound<LOW_BITS<TYPE>>(sh, p.top);
     each([&](uint32_t key, uint32_t cls) {
         if (key >= bound) {
             const uint32_t at = atomicAdd(&sh.listed, 1u);
@@ -484,7 +530,7 @@ RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, bool sm
     cut.chunks = chunks_of(cut.nv);
     cut.chunk_vecs = (vecs + cut.chunks - 1) / cut.chunks;
     cut.chunks = (vecs + cut.chunk_vecs - 1) / cut.chunk_vecs;   // none of them empty
-    cut.list_cap = cut.chunks == 1 ? LIST : 2 * top + 64;
+    cut.list_cap = cut.chunks == 1 ? LIST : std::max(128u, 2 * top + 64);
     cut.rows = (uint32_t)std::min<uint64_t>(rows, std::max<uint32_t>(1, most / cut.chunks));
     cut.parts_bytes = cut.chunks == 1 ? 0 : ((size_t)cut.rows * cut.chunks * sizeof(Part) + 255) / 256 * 256;
     cut.lists_bytes = cut.chunks == 1 || !top ? 0 : (size_t)cut.rows * cut.chunks * cut.list_cap * sizeof(uint2);
