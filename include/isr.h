@@ -189,7 +189,8 @@ size_t isr_noise_bank_static_capacity(void);
  * equal bits; the last bits of a row's sums may depend on the number of rows and on whether the
  * row starts at an even or an odd element.
  *
- * Logits x[r][j], j < classes, element (r, j) at data_device + r * row_stride + j (in elements);
+ * Results and workspace overlap neither each other nor what a call reads, but for gradients over
+ * the logits.  Logits x[r][j], j < classes, element (r, j) at data_device + r * row_stride + j (in elements);
  * aligned to their element, no more.  l = scale * x: scale is 1 / temperature, times the step of
  * one unit for int32 logits of an int8 network.  A float logit of -infinity marks an impossible
  * class.  A row without a possible class is empty.  A row that holds NaN or +infinity has NaN as
@@ -205,7 +206,7 @@ typedef struct isr_logits {
     uint32_t classes;    /* 1 .. 2^24 */
     uint64_t rows;       /* 0 .. 2^31 - 1 */
     uint64_t row_stride; /* elements, >= classes */
-    float scale;         /* finite, > 0 */
+    float scale;         /* 1e-30 .. 1e30 */
 } isr_logits;
 
 #define ISR_MAX_GIVEN 128 /* given classes a row, and entries of the teacher */
@@ -252,7 +253,7 @@ typedef struct isr_teacher {
     const void *logit_device;    /* [rows][top] */
     int32_t type;                /* ISR_F32, ISR_BF16 or ISR_F16 */
     uint32_t top;                /* 1 .. ISR_MAX_GIVEN */
-    float scale;                 /* finite, > 0 */
+    float scale;                 /* 1e-30 .. 1e30 */
     int32_t rest;
 } isr_teacher;
 

@@ -1,6 +1,6 @@
 // Entry points of the operators on rows of class logits: arguments are checked here, on the host, and the kernels
 // rely on it.  Nothing is allocated, copied or waited for.
-#include <cmath>
+#include <initializer_list>
 
 #include "logit_rows.h"
 
@@ -12,7 +12,7 @@ constexpr uint32_t MAX_CLASSES = 1u << 24;
 
 size_t element_bytes(int type) { return type == ISR_F32 || type == ISR_I32 ? 4 : 2; }
 bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
-bool usable_scale(float s) { return std::isfinite(s) && s > 0.f; }
+bool usable_scale(float s) { return s >= 1e-30f && s <= 1e30f; }   // its product with log2 e too is a normal number; not NaN
 
 // shapes and type, what the size of a workspace depends on
 bool valid_shape(const isr_logits *l) {

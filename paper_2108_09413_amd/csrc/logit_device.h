@@ -198,7 +198,7 @@ struct Chunk {
         // none of these in a branch, behind whose end the compiler would wait for all that is in flight
 #pragma unroll
         for (int i = 0; i < NV; ++i) raw[i] = ((const Loose *)(x + head + (size_t)min(v0 + i * T + threadIdx.x, final_vec) * PV))->v;
-        edge = x[last ? min(beside, l.classes - 1) : head];   // of use where edge_valid
+        edge = x[last ? min(beside, l.classes - 1) : head + min(v0, vecs - 1) * PV];   // of use where edge_valid
     }
     __device__ __forceinline__ bool owns(uint32_t j) const { return j - first < n * PV || (last && (j < head || j >= end)); }   // j below the number of classes
     __device__ __forceinline__ bool has(int i) const { return i * T + threadIdx.x < n; }

@@ -131,6 +131,59 @@ def test_many_rows(isr, torch, kind, rows, classes, top):
     check_grad(isr, torch, kind, dev, wide, scale_of(kind), given, rng.normal(size=(rows, 2)), rng.normal(size=rows), r)
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+@pytest.mark.parametrize("classes", [5, 100, 256, 257, 3001, 20011])
+@pytest.mark.parametrize("n", [64, 65, 128])
+def test_many_given_classes_with_repetitions(isr, torch, kind, classes, n):
+    """The given of up to 128, of few different classes, so that many name one; in place as well."""
+    rng = np.random.default_rng(n)
+    dev, wide = make(torch, kind, 3, classes, n, pad=1)
+    some = rng.integers(0, classes, 20)
+    given = np.where(rng.random((3, n)) < 0.1, -1, rng.choice(some, (3, n)))
+    r = check_logprobs(isr, torch, kind, dev, wide, 1.0, given, 1)
+    up = rng.normal(size=(3, n))
+    check_grad(isr, torch, kind, dev, wide, 1.0, given, up, None, r)
+    check_grad(isr, torch, kind, dev, wide, 1.0, given, up, up[:, 0], r, out=dev)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("classes", [10, 200, 5003, 50021])
+def test_each_result_alone(isr, torch, kind, classes):
+    dev, wide = make(torch, kind, 3, classes, classes, shift=1)
+    scale, given = scale_of(kind), np.array([[1, -1], [0, 0], [classes - 1, 2]])
+    g = torch.from_numpy(given.astype(np.int32)).cuda()
+    lp, h, tc, tl = plain.logprobs(wide, scale, given, 9)
+    a = isr.isr_logprobs(dev, g, scale=scale)
+    assert a.entropy is a.top is a.top_class is a.stats is None
+    close(a.given, lp, plain.logp_tol(lp), "given")
+    b = isr.isr_logprobs(dev, entropy=True, scale=scale)
+    assert b.given is None
+    close(b.entropy, h, plain.U * plain.SUM * (3 + 2 * math.log(classes)), "entropy")
+    c = isr.isr_logprobs(dev, top=9, scale=scale)
+    close(c.top, tl, plain.logp_tol(tl), "top")
+    assert np.array_equal(c.top_class.cpu().numpy(), tc)
+    d = isr.isr_logprobs(dev, stats=True, scale=scale)
+    up = np.ones((3, 2))
+    check_grad(isr, torch, kind, dev, wide, scale, given, up, None, d)
+
+
+def test_more_rows_than_a_launch_takes(isr, torch):
+    """Behind 2^22 workgroups the next launch goes on: rows on both sides against the same rows by themselves."""
+    for classes, rows in ((260, (1 << 22) + 5), (1, (1 << 26) + 5)):
+        print(classes, rows, flush=True)
+        x = torch.randn((rows, classes), device="cuda", dtype=torch.bfloat16)
+        e = torch.zeros((rows, 1), device="cuda", dtype=torch.int32)
+        v = torch.full((rows, 1), -0.5, device="cuda")
+        at = torch.tensor([0, 1, (1 << 22) - 1, 1 << 22, rows - 2, rows - 1])
+        few = x[at].contiguous()
+        r, s = (isr.isr_logprobs(z, e[:len(z)], top=1, entropy=True, stats=True) for z in (x, few))
+        d, f = (isr.isr_distill(z, e[:len(z)], v[:len(z)], rest=True, grad=True) for z in (x, few))
+        g, h = (isr.isr_logprobs_grad(z, e[:len(z)], v[:len(z)], q.stats) for z, q in ((x, r), (few, s)))
+        for big, small in zip([*r, d.loss, d.grad, g], [*s, f.loss, f.grad, h]):
+            assert torch.equal(big[at], small)
+        assert bool((r.top_class >= 0).all()) and bool(torch.isfinite(r.given).all()) and bool(torch.isfinite(d.loss).all() or classes == 1)
+
+
 def special_rows(kind, classes, rng):
     """Rows that a mask or a broken model leaves, name by name."""
     big = {"f32": np.finfo(np.float32).max, "bf16": 2.0 ** 127 * (2 - 2.0 ** -7), "f16": 65504.0, "i32": 2.0 ** 31 - 1}[kind]

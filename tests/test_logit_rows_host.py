@@ -42,7 +42,7 @@ def _distill_grad(l, t, w=P[0], st=P[1], out=P[2], stride=104):
 
 BAD_LOGITS = [dict(data=None), dict(data=BASE + 1), dict(kind=4), dict(kind=-1), dict(classes=0), dict(classes=(1 << 24) + 1, stride=1 << 25),
               dict(rows=1 << 31), dict(stride=99), dict(stride=1 << 62), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf),
-              dict(scale=math.nan), dict(kind=isr.F32, data=BASE + 2)]
+              dict(scale=math.nan), dict(scale=1e-31), dict(scale=2e30), dict(kind=isr.F32, data=BASE + 2)]
 
 
 @pytest.mark.parametrize("bad", BAD_LOGITS, ids=str)
