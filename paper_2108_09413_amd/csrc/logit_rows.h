@@ -19,6 +19,7 @@ struct RowCut {
     uint32_t chunk_vecs;   // vectors of a chunk, the last one's may be fewer
     uint32_t list_cap;     // room for candidates of the top alternatives, of a chunk
     uint32_t rows;         // of a launch
+    bool whole;            // a workgroup goes through all chunks of a row
     size_t parts_bytes, lists_bytes;
 };
 bool small_rows(uint32_t classes, uint32_t serial);
@@ -37,6 +38,7 @@ struct LogprobsParams {
     uint64_t row0;
     uint32_t run;             // rows
     uint32_t chunks, chunk_vecs, list_cap;
+    bool whole;
     Part *parts;
     uint2 *lists;
 };

@@ -315,6 +315,148 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
         for (uint32_t i = tid; i < sh.listed; i += THREADS) p.lists[at * p.list_cap + i] = sh.list[i];
 }
 
+// Many rows with top alternatives: a workgroup goes through its row chunk by chunk, and no join is needed.  The bound of the
+// first chunk serves until the listed vectors may want room; then, and at the end, it is raised to what `top` of the listed
+// reach, and those below are dropped.  A chunk with more than there is room for (a row that ascends) raises it to its own; rows with
+// more candidates all the same (of many equal logits) are searched in memory.
+// us of a call with 20 / 64 / 128 alternatives, by chunks and join -> this way: 2048 x 32000 bf16 38 / 49 / 89 -> 33 / 39 / 47,
+// 2048 x 32771 f32 56 / 61 / 74 -> 47 / 54 / 63, 4096 x 131072 bf16 210 / 222 / 244 -> 197 / 235 / 247.  So: enough rows for four
+// workgroups a CU, and few alternatives or few chunks.
+constexpr uint64_t WHOLE_ROWS = 1024;
+constexpr uint32_t WHOLE_TOP = 32, WHOLE_CHUNKS = 5;
+template <int TYPE, int NV, bool ENT>
+__global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const LogprobsParams p) {
+    using K = Kind<TYPE>;
+    using Val = typename K::Val;
+    constexpr int PV = PER_VEC<TYPE>, OWN = VECS / THREADS;
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    __shared__ __attribute__((aligned(16))) SharedVecs vecs;
+    const uint32_t tid = threadIdx.x;
+    const uint64_t r = p.row0 + blockIdx.x;
+    const float c = p.l.scale * LOG2E;
+    Stat<Val> a{lowest(Val()), 0.f, 0.f};
+    Val from = of_key<Val>(least_key<Val>());
+    bool lost = false;     // candidates that found no room; this and the next are the same for all threads
+    uint32_t listed = 0, added = 0;
+    if (tid == 0) sh.listed = vecs.listed = 0;
+    auto most_of = [](const Val (&v)[PV]) __attribute__((always_inline)) {
+        Val m = v[0];
+#pragma unroll
+        for (int e = 1; e < PV; ++e) m = larger(m, v[e]);
+        return m;
+    };
+    auto raise = [&](uint32_t key) __attribute__((always_inline)) {   // to what `top` of the threads' keys reach; a barrier
+        sh.key[tid] = key;
+        __syncthreads();
+        from = larger(from, of_key<Val>(max(key_bound<LOW_BITS<TYPE>>(sh, p.top), least_key<Val>())));
+    };
+    auto raise_by_listed = [&](Val (&most)[OWN]) __attribute__((always_inline)) {
+        uint32_t key = 0;
+#pragma unroll
+        for (int h = 0; h < OWN; ++h) {
+            Val v[PV];
+            unpack<TYPE>(vecs.raw[tid + h * THREADS], v);
+            most[h] = most_of(v);
+            if (tid + h * THREADS < listed) key = max(key, key_of(most[h]));
+        }
+        raise(key);
+    };
+    Val edge = lowest(Val());
+    uint32_t edge_class = 0;
+    bool edge_valid = false;
+    for (uint32_t chunk = 0; chunk < p.chunks; ++chunk) {
+        if (listed + added + added / 2 + 40 > VECS && !lost) {   // if the next chunk adds what the last one did, and many deviations more
+            Val most[OWN];
+            typedef uint32_t Words __attribute__((ext_vector_type(4)));
+            Words raw[OWN];
+            uint32_t first[OWN];
+            raise_by_listed(most);
+#pragma unroll
+            for (int h = 0; h < OWN; ++h) {
+                raw[h] = ((const Words *)vecs.raw)[tid + h * THREADS];
+                first[h] = vecs.first[tid + h * THREADS];
+            }
+            if (tid == 0) vecs.listed = 0;
+            __syncthreads();
+#pragma unroll
+            for (int h = 0; h < OWN; ++h) {
+                const bool stays = tid + h * THREADS < listed && !(most[h] < from);
+                const uint64_t of = __ballot(stays);
+                const uint32_t at = places(__popcll(of), &vecs.listed) + lanes_before(of);
+                if (stays) { ((Words *)vecs.raw)[at] = raw[h]; vecs.first[at] = first[h]; }
+            }
+            __syncthreads();
+            listed = vecs.listed;
+        }
+        Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+        Val most[NV], m = lowest(Val());
+        k.each([&](int i, uint32_t, const Val (&v)[PV]) {
+            most[i] = most_of(v);
+            m = larger(m, most[i]);
+        });
+        k.keep_packed();
+        edge = K::val(k.edge);
+        edge_class = k.beside;
+        edge_valid = k.edge_valid;
+        refer(a, larger(a.m, edge_valid ? larger(m, edge) : m), c);
+        auto add = [&](Val v) {
+            const float d = c * below(v, a.m), e = __builtin_amdgcn_exp2f(d);
+            a.s += e;
+            if (ENT) a.t += e * fmaxf(d, NO_SHARE);
+        };
+        if (edge_valid) add(edge);
+        k.each([&](int, uint32_t, const Val (&v)[PV]) {
+#pragma unroll
+            for (int e = 0; e < PV; ++e) add(v[e]);
+        });
+        k.keep_packed();
+        if (chunk == 0) raise(key_of(m));
+        else __syncthreads();   // all have read the count
+        for (bool again = false;; again = true) {
+            list_vectors(k, most, from, vecs);
+            __syncthreads();
+            const uint32_t n = vecs.listed;
+            if (n <= VECS || again || lost) {
+                lost = lost || n > VECS;
+                added = min(n, (uint32_t)VECS) - listed;
+                listed += added;
+                break;
+            }
+            raise(key_of(m));
+            if (tid == 0) vecs.listed = listed;
+            __syncthreads();
+        }
+    }
+    Given<TYPE> given;
+    given.load(p, r);
+    const Stat<Val> all = block_stat<THREADS, ENT>(a, c, sh, [] {});
+    Val most[OWN];
+    raise_by_listed(most);
+    list_element(edge_valid, edge, edge_class, from, sh);
+    list_elements<TYPE>(vecs, from, sh);
+    __syncthreads();
+    if (lost || sh.listed > LIST) {
+        __syncthreads();
+        const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+        const uint32_t whole = p.l.classes / PV * PV;
+        list_exactly([&](auto f) {
+            for (uint32_t j = tid * PV; j < whole; j += THREADS * PV) {
+                Val v[PV];
+                unpack<TYPE>(((const Loose *)(x + j))->v, v);
+#pragma unroll
+                for (int e = 0; e < PV; ++e)
+                    if (possible(v[e])) f(key_of(v[e]), j + e);
+            }
+            if (whole + tid < p.l.classes) {
+                const Val v = K::val(x[whole + tid]);
+                if (possible(v)) f(key_of(v), whole + tid);
+            }
+        }, p.top, sh);
+    }
+    finish_values<TYPE>(p, r, all, given);
+    finish_top<TYPE>(p, r, all, sh);
+}
+
 // The chunks of a row together: without top alternatives by a wave, with them by a workgroup.
 template <int TYPE>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(const LogprobsParams p) {
@@ -530,8 +672,10 @@ RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, bool sm
     cut.chunks = chunks_of(cut.nv);
     cut.chunk_vecs = (vecs + cut.chunks - 1) / cut.chunks;
     cut.chunks = (vecs + cut.chunk_vecs - 1) / cut.chunk_vecs;   // none of them empty
+    cut.whole = top && cut.chunks > 1 && rows >= WHOLE_ROWS && (top <= WHOLE_TOP || cut.chunks <= WHOLE_CHUNKS);
     cut.list_cap = cut.chunks == 1 ? LIST : std::max(128u, 2 * top + 64);
     cut.rows = (uint32_t)std::min<uint64_t>(rows, std::max<uint32_t>(1, most / cut.chunks));
+    if (cut.whole) return cut;
     cut.parts_bytes = cut.chunks == 1 ? 0 : ((size_t)cut.rows * cut.chunks * sizeof(Part) + 255) / 256 * 256;
     cut.lists_bytes = cut.chunks == 1 || !top ? 0 : (size_t)cut.rows * cut.chunks * cut.list_cap * sizeof(uint2);
     return cut;
@@ -580,11 +724,16 @@ static void launch_small(const Params &p, hipStream_t st) {
 template <int TYPE>
 static void launch_rows(const LogprobsParams &p, uint32_t nv, hipStream_t st) {
     if (nv == 0) return launch_small<TYPE>(p, st);
+    const dim3 grid(p.run), block(THREADS);
+    if (p.whole) {
+        if (p.entropy) hipLaunchKernelGGL((logprobs_row_top_kernel<TYPE, 8, true>), grid, block, 0, st, p);
+        else hipLaunchKernelGGL((logprobs_row_top_kernel<TYPE, 8, false>), grid, block, 0, st, p);
+        return;
+    }
     if (nv == 2) launch_chunks<TYPE, 2>(p, st);
     else if (nv == 4) launch_chunks<TYPE, 4>(p, st);
     else launch_chunks<TYPE, 8>(p, st);
     if (p.chunks == 1) return;
-    const dim3 grid(p.run), block(THREADS);
     if (!p.top) hipLaunchKernelGGL((logprobs_join_kernel<TYPE>), grid, dim3(64), 0, st, p);
     else if (p.chunks <= 16 && p.list_cap <= 128) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 2>), grid, block, 0, st, p);
     else if (p.chunks <= 8 && p.list_cap <= 256) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 4>), grid, block, 0, st, p);
@@ -598,6 +747,7 @@ hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace,
     p.chunks = cut.chunks;
     p.chunk_vecs = cut.chunk_vecs;
     p.list_cap = cut.list_cap;
+    p.whole = cut.whole;
     p.parts = (Part *)workspace;
     p.lists = (uint2 *)((uint8_t *)workspace + cut.parts_bytes);
     return by_runs(p, cut.rows, [&](uint32_t rows) {

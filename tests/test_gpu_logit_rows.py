@@ -167,6 +167,44 @@ def test_each_result_alone(isr, torch, kind, classes):
     check_grad(isr, torch, kind, dev, wide, scale, given, up, None, d)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("classes,top", [(16400, 128), (20011, 20), (40007, 64), (40007, 1)])
+def test_top_alternatives_of_many_long_rows(isr, torch, kind, classes, top):
+    """Rows that a workgroup goes through by chunks: ordinary ones, ascending ones (each chunk beats the last), descending, of few
+    values, of one, with few possible classes, empty, with NaN; every row's classes against a stable sort."""
+    rows = 1100
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(classes + top)
+    x = torch.randn((rows, classes), generator=gen, device="cuda") * 3
+    x[7] = x[7].sort().values
+    x[8] = x[8].sort(descending=True).values
+    x[9] = x[9].round()
+    x[10] = 1.5
+    x[11:40] += torch.linspace(0, 40, classes, device="cuda")
+    x[40, classes // 2:] = 30
+    if kind == "i32":
+        x = (x * 1000).round().to(torch.int32)
+        x[12] = torch.iinfo(torch.int32).min
+    else:
+        x[13] = -math.inf
+        x[14, top // 2 + 1:] = -math.inf
+        x[15, 5:classes - 3] = -math.inf
+        x[16, classes - 1] = math.nan
+        x = x.to(dtype_of(torch, kind))
+    r = isr.isr_logprobs(x, top=top, entropy=True, scale=scale_of(kind))
+    wide = x.double()
+    value, index = torch.sort(wide, dim=1, descending=True, stable=True)
+    index[value == -math.inf] = -1
+    index = index[:, :top].to(torch.int32)
+    if kind != "i32":
+        index[16] = -1
+    assert torch.equal(r.top_class, index)
+    some = [0, 7, 8, 9, 10, 12, 13, 14, 15, 16, 17, 39, 40, rows - 1]
+    _, h, _, tl = plain.logprobs(wide[some].cpu().numpy(), scale_of(kind), None, top)
+    close(r.top[some], tl, plain.logp_tol(tl), "top log-probabilities")
+    close(r.entropy[some], h, plain.U * plain.SUM * (3 + 2 * math.log(classes)), "entropy")
+
+
 def test_more_rows_than_a_launch_takes(isr, torch):
     """Behind 2^22 workgroups the next launch goes on: rows on both sides against the same rows by themselves."""
     for classes, rows in ((260, (1 << 22) + 5), (1, (1 << 26) + 5)):
