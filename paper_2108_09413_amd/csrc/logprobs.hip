@@ -2,8 +2,10 @@
 //
 // Forward: a row is cut into chunks of up to 256 * NV vectors of 16 bytes, one workgroup each, which holds its chunk in
 // registers: one pass over memory, then maximum, exponentials and candidates of the top alternatives from registers.  The
-// chunks' results meet in a second launch (join), or in the same one where a row is one chunk.  Bound by memory: 4096 rows of
-// 131072 bf16 in 182 us, 5.9 TB/s.
+// chunks' results meet in a second launch (join), or in the same one where a row is one chunk; of many rows with top
+// alternatives a workgroup goes through all chunks of one.  Bound by memory: 4096 rows of 131072 bf16 in 182 us, 5.9 TB/s,
+// with 20 alternatives in 197.  Few rows are bound by latency: one row of 131072 with 20 alternatives takes 6.8 us for
+// the chunks and 6.0 for the join.
 // Gradient: element by element from the row's statistics, bound by memory too: 2048 x 65537 bf16 in 97 us, 5.5 TB/s; the few
 // named classes are stored behind the others.
 // Rows of up to 256 classes go by 16 lanes each.
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
         list_elements<TYPE>(vecs, from, sh);
         if (vecs.listed > VECS && tid == 0) atomicMax(&sh.listed, LIST + 1u);   // some are missing: more than fit
         __syncthreads();
-        const uint32_t listed = sh.listed;   // uniform
+        const uint32_t listed = all.s == all.s ? sh.listed : 0;   // uniform; of a row with NaN nothing is asked for
         if (listed > p.list_cap && listed <= LIST) {   // neighbours that reach the bound together: of the listed, two a thread
             const uint2 mine[2] = {tid < listed ? sh.list[tid] : make_uint2(0, 0), tid + THREADS < listed ? sh.list[tid + THREADS] : make_uint2(0, 0)};
             __syncthreads();
@@ -310,9 +312,10 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
         return;
     }
     const size_t at = (size_t)row * p.chunks + chunk;
-    if (tid == 0) p.parts[at] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, all.t, TOP ? sh.listed : 0};
+    const uint32_t n = TOP && all.s == all.s ? sh.listed : 0;   // at most list_cap by now
+    if (tid == 0) p.parts[at] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, all.t, n};
     if constexpr (TOP)
-        for (uint32_t i = tid; i < sh.listed; i += THREADS) p.lists[at * p.list_cap + i] = sh.list[i];
+        for (uint32_t i = tid; i < n; i += THREADS) p.lists[at * p.list_cap + i] = sh.list[i];
 }
 
 // Many rows with top alternatives: a workgroup goes through its row chunk by chunk, and no join is needed.  The bound of the
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
     list_element(edge_valid, edge, edge_class, from, sh);
     list_elements<TYPE>(vecs, from, sh);
     __syncthreads();
-    if (lost || sh.listed > LIST) {
+    if ((lost || sh.listed > LIST) && all.s == all.s) {   // of a row with NaN nothing is asked for
         __syncthreads();
         const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
         const uint32_t whole = p.l.classes / PV * PV;
