@@ -346,27 +346,25 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = K::val(x[min(lane + 16 * i, n - 1)]);
     const float w = p.weight ? p.weight[r] : 1.f, c = p.l.scale * LOG2E;
-    // the entries, up to 8 a lane
-    constexpr int B = ISR_MAX_GIVEN / 16;
-    int32_t ec[B];
-    float ev[B];
+    // the entries: each lane every sixteenth, then in LDS for all of the row's
+    __shared__ int32_t entries[THREADS / 16][ISR_MAX_GIVEN];
+    __shared__ float shares[THREADS / 16][ISR_MAX_GIVEN];
+    int32_t *const ec = entries[threadIdx.x >> 4];
+    float *const eq = shares[threadIdx.x >> 4];   // the teacher's value, then q
     float value_m = NEG_INF;
     int any = 0, bad = 0;
-#pragma unroll
-    for (int b = 0; b < B; ++b) {
-        ec[b] = -1;
-        ev[b] = NEG_INF;
-        if (b * 16 >= p.top) continue;   // uniform
-        const uint32_t i = lane + 16 * b;
-        if (i < p.top) ec[b] = p.entry[r * p.top + i];
-        if (ec[b] >= 0) ev[b] = teacher_value(p.value, p.value_type, r * p.top + i);
-        any |= ec[b] >= 0;
-        bad |= ec[b] >= 0 && ((uint32_t)ec[b] >= n || ev[b] != ev[b] || ev[b] == -NEG_INF);
-        value_m = larger(value_m, ev[b]);
+    for (uint32_t i = lane; i < p.top; i += 16) {
+        const int32_t cls = p.entry[r * p.top + i];
+        const float value = cls >= 0 ? teacher_value(p.value, p.value_type, r * p.top + i) : NEG_INF;
+        ec[i] = cls;
+        eq[i] = value;
+        any |= cls >= 0;
+        bad |= cls >= 0 && ((uint32_t)cls >= n || value != value || value == -NEG_INF);
+        value_m = larger(value_m, value);
     }
     DistillStat st;
     if constexpr (!FORWARD) st = p.stats[r];
-    float value_logs;
+    float value_logs = 0.f;
     double left = 0.0, total = 0.0, entropy = 0.0;   // q_rest, sum of q, sum of q log q
     bool none = false;
     if constexpr (FORWARD) {
@@ -375,49 +373,43 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
         value_m = p.rest ? 0.f : max16(value_m);
         none = !any || value_m == NEG_INF;
         if (none) value_m = 0.f;
-        value_logs = 0.f;
         if (!p.rest) {
             float z = 0.f;
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-                if (b * 16 < p.top) z += ec[b] >= 0 ? expf(p.value_scale * (ev[b] - value_m)) : 0.f;
+            for (uint32_t i = lane; i < p.top; i += 16) z += ec[i] >= 0 ? expf(p.value_scale * (eq[i] - value_m)) : 0.f;
             value_logs = logf(sum16(z));
         }
     } else {
         value_m = st.value_m;
         value_logs = st.value_logs;
     }
+    for (uint32_t i = lane; i < p.top; i += 16) {
+        float share = 0.f;
+        if (ec[i] >= 0) {
+            if (FORWARD && p.rest) {   // the sum that leads to q_rest in 64 bits
+                const double lq = (double)p.value_scale * (double)eq[i], full = exp(lq);
+                total += full;
+                share = (float)full;
+                if (share > 0.f) entropy += (double)share * lq;
+            } else {
+                const float lq = p.value_scale * (eq[i] - value_m) - value_logs;
+                share = expf(lq);
+                if (FORWARD && share > 0.f) { total += share; entropy += (double)share * lq; }
+            }
+        }
+        eq[i] = share;
+    }
+    wave_order();
     // sum of q by class: every lane sees all entries in turn and keeps those of its elements
     float q[E] = {};
     uint32_t member = 0;
+    for (uint32_t i = 0; i < p.top; ++i) {
+        const int32_t cls = ec[i];
+        const float share = eq[i];
+        const int own = cls >= 0 && (cls & 15) == (int)lane ? cls >> 4 : -1;
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-        if (b * 16 >= p.top) continue;
-        float qb = 0.f;
-        if (ec[b] >= 0) {
-            if (FORWARD && p.rest) {
-                const double lq = (double)p.value_scale * (double)ev[b], full = exp(lq);
-                total += full;
-                qb = (float)full;
-                if (qb > 0.f) entropy += (double)qb * lq;
-            } else {
-                const float lq = p.value_scale * (ev[b] - value_m) - value_logs;
-                qb = expf(lq);
-                if (FORWARD && qb > 0.f) { total += qb; entropy += (double)qb * lq; }
-            }
-        }
-        const uint32_t some = min(16u, p.top - b * 16);
-        for (uint32_t i = 0; i < some; ++i) {
-            const int from = (threadIdx.x & 48) | i;
-            const int cls = __shfl(ec[b], from, 64);
-            const float share = __shfl(qb, from, 64);
-            if (cls < 0 || (cls & 15) != (int)lane) continue;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (cls >> 4 != e) continue;
-                q[e] += share;
-                member |= 1u << e;
-            }
+        for (int e = 0; e < E; ++e) {
+            q[e] += own == e ? share : 0.f;
+            member |= (uint32_t)(own == e) << e;
         }
     }
     if constexpr (FORWARD) {
@@ -499,6 +491,7 @@ static void launch_small(const DistillParams &p, hipStream_t st) {
     const dim3 grid((p.run + THREADS / 16 - 1) / (THREADS / 16)), block(THREADS);
     if (p.l.classes <= 16) hipLaunchKernelGGL((distill_small_kernel<TYPE, 1, FORWARD>), grid, block, 0, st, p);
     else if (p.l.classes <= 64) hipLaunchKernelGGL((distill_small_kernel<TYPE, 4, FORWARD>), grid, block, 0, st, p);
+    else if (p.l.classes <= 128) hipLaunchKernelGGL((distill_small_kernel<TYPE, 8, FORWARD>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((distill_small_kernel<TYPE, 16, FORWARD>), grid, block, 0, st, p);
 }
 

@@ -721,6 +721,7 @@ template <int TYPE, class Params>
 static void launch_small(const Params &p, hipStream_t st) {
     if (p.l.classes <= 16) launch_small<TYPE, 1>(p, st);
     else if (p.l.classes <= 64) launch_small<TYPE, 4>(p, st);
+    else if (p.l.classes <= 128) launch_small<TYPE, 8>(p, st);
     else launch_small<TYPE, 16>(p, st);
 }
 
