@@ -5,7 +5,7 @@
 // Both at once, rows that fit the registers of a workgroup (up to 16384 vectors of 16 bytes): the row is read once, held, and
 // its gradient stored from there, 4096 x 131072 bf16 with 64 entries and rest in 434 us (4.95 TB/s, of 5.8 that the
 // gradient alone reaches), 8192 x 32000 in 199 (5.3).  Longer rows take the two ways one after the other.
-// Rows of up to 256 classes go by 16 lanes each.
+// Rows of up to 256 classes go by 16 lanes each unless they have many entries; rows of up to 256 vectors by a single wave.
 #include <algorithm>
 
 #include "logit_device.h"
@@ -143,6 +143,7 @@ __device__ __forceinline__ DistillStat conclude(const DistillParams &p, uint64_t
         if (t.q[h] > 0.f) loss += (double)t.q[h] * (t.logq(p, e.v[h]) - lp);
     }
     loss = wave_sum(loss);
+    if (!p.rest) loss /= t.total;   // the q are rounded to 24 bits, and a sum of theirs above 1 would take a loss near the largest number to infinity
     if (t.left > 0.0) {
         const double lr = a.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(a.m, all.m) + ((double)rest_logs - logs);
         loss += t.left * (logf((float)t.left) - lr);
@@ -171,13 +172,13 @@ __device__ __forceinline__ float entry_slope(const DistillParams &p, const Disti
     return p.l.scale * w * (st.total * __builtin_amdgcn_exp2f(p.l.scale * LOG2E * below(x, of_bits<Val>(st.m)) - st.logs * LOG2E) - q);
 }
 
-template <int TYPE, int NV>
-__global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillParams p) {
+template <int TYPE, int T, int NV>
+__global__ __launch_bounds__(T) void distill_grad_kernel(const DistillParams p) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     const uint32_t row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks, lane = threadIdx.x & 63;
     const uint64_t r = p.row0 + row;
-    const Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+    const Chunk<TYPE, T, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
     const DistillStat st = p.stats[r];
     const float w = p.weight ? p.weight[r] : 1.f;
     Named named;
@@ -194,8 +195,17 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillPara
 template <bool REST, int T, int NV> struct SharedMask { uint32_t bits[NV * T / 4], tail; };
 template <int T, int NV> struct SharedMask<false, T, NV> {};
 
+template <int T>
+struct RowEntries {   // of the row, one a thread, two of a single wave
+    int32_t c[T == 64 ? 2 : 1];
+    __device__ __forceinline__ RowEntries(const DistillParams &p, uint64_t r) {
+#pragma unroll
+        for (uint32_t h = 0; h < sizeof(c) / 4; ++h) c[h] = threadIdx.x + h * T < p.top ? p.entry[r * p.top + threadIdx.x + h * T] : -1;
+    }
+};
+
 template <bool REST, int TYPE, int T, int NV>
-__device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(Chunk<TYPE, T, NV> &k, uint32_t classes, float c, int32_t entry, SharedMask<REST, T, NV> &sh) {
+__device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(Chunk<TYPE, T, NV> &k, uint32_t classes, float c, const RowEntries<T> &entries, SharedMask<REST, T, NV> &sh) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>, WORDS = (NV + 3) / 4;
@@ -208,7 +218,9 @@ __device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(Chunk<TYPE,
             if (i * T + tid < NV * T / 4) sh.bits[i * T + tid] = 0;
         if (tid == 0) sh.tail = 0;
         __syncthreads();
-        if ((uint32_t)entry < classes && k.owns((uint32_t)entry)) {   // not negative either
+#pragma unroll
+        for (const int32_t entry : entries.c) {
+            if ((uint32_t)entry >= classes || !k.owns((uint32_t)entry)) continue;   // or negative
             const uint32_t j = (uint32_t)entry - k.first;
             if (j < k.n * PV) {
                 const uint32_t vec = j / PV, byte = vec % T * NV + vec / T;
@@ -253,19 +265,19 @@ __device__ __forceinline__ Stat<typename Kind<TYPE>::Val> chunk_stat(Chunk<TYPE,
 }
 
 // A chunk of a row, or (p.chunks == 1) a whole one.
-template <int TYPE, int NV, bool REST>
-__global__ __launch_bounds__(THREADS) void distill_kernel(const DistillParams p) {
+template <int TYPE, int T, int NV, bool REST>
+__global__ __launch_bounds__(T) void distill_kernel(const DistillParams p) {
     using Val = typename Kind<TYPE>::Val;
-    __shared__ SharedStat<THREADS> sh;
-    __shared__ SharedMask<REST, THREADS, NV> mask;
+    __shared__ SharedStat<T> sh;
+    __shared__ SharedMask<REST, T, NV> mask;
     __shared__ __attribute__((aligned(16))) uint32_t table[SLOTS];
     const uint32_t tid = threadIdx.x, row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks;
     const uint64_t r = p.row0 + row;
     // in front of the row's loads, behind which it would have to wait for them
-    const int32_t entry = REST && tid < p.top ? p.entry[r * p.top + tid] : -1;
-    Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+    const RowEntries<T> entries(p, r);
+    Chunk<TYPE, T, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
     const float c = p.l.scale * LOG2E;
-    const Stat<Val> all = block_stat<THREADS, false>(chunk_stat<REST>(k, p.l.classes, c, entry, mask), c, sh, [] {});
+    const Stat<Val> all = block_stat<T, false>(chunk_stat<REST>(k, p.l.classes, c, entries, mask), c, sh, [] {});
     if (p.chunks > 1) {
         if (tid == 0) p.parts[(size_t)row * p.chunks + chunk] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, 0.f, 0};
         return;
@@ -300,7 +312,7 @@ __global__ __launch_bounds__(T) void distill_row_kernel(const DistillParams p) {
     __shared__ DistillStat stat;
     const uint32_t tid = threadIdx.x;
     const uint64_t r = p.row0 + blockIdx.x;
-    const int32_t entry = REST && tid < p.top ? p.entry[r * p.top + tid] : -1;
+    const RowEntries<T> entries(p, r);
     Entries<TYPE> e;
     if (tid < 64) e.load(p, r);
     const float w = p.weight ? p.weight[r] : 1.f;
@@ -308,7 +320,7 @@ __global__ __launch_bounds__(T) void distill_row_kernel(const DistillParams p) {
     Taught t;
     if (tid < 64) t = taught<TYPE>(p, e, table);   // while the row arrives
     const float c = p.l.scale * LOG2E;
-    const Stat<Val> all = block_stat<T, false>(chunk_stat<REST>(k, p.l.classes, c, entry, mask), c, sh, [] {});
+    const Stat<Val> all = block_stat<T, false>(chunk_stat<REST>(k, p.l.classes, c, entries, mask), c, sh, [] {});
     if (tid < 64) {
         const DistillStat st = conclude<TYPE>(p, r, all, e, t);
         if (tid == 0) {
@@ -447,6 +459,7 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
             cross += (double)q[i] * (empty || !possible(v[i]) ? (double)NEG_INF : (double)p.l.scale * below64(v[i], all.m) - logs);
         }
         double loss = entropy - sum16(cross);
+        if (!p.rest) loss /= total;   // as in conclude()
         if (left > 0.0) {
             const double lr = a.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(a.m, all.m) + ((double)rest_logs - logs);
             loss += left * (logf((float)left) - lr);
@@ -474,11 +487,8 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
 // ---- launches --------------------------------------------------------------------------------
 
 static uint32_t vecs_of(int type, uint32_t classes) { return classes / (type == ISR_F32 || type == ISR_I32 ? 4 : 8); }
-static bool small(uint32_t classes, uint32_t top) { return small_rows(classes, top); }
 
-bool distill_in_one(int type, uint32_t classes, uint32_t top) { return small(classes, top) || vecs_of(type, classes) <= 16 * 1024; }
-
-RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top) { return cut_rows(type, classes, rows, 0, small(classes, top)); }
+bool distill_in_one(int type, uint32_t classes) { return vecs_of(type, classes) <= 16 * 1024; }
 
 template <int TYPE, int T, int NV>
 static void launch_row_kernel(const DistillParams &p, hipStream_t st) {
@@ -495,13 +505,17 @@ static void launch_small(const DistillParams &p, hipStream_t st) {
     else hipLaunchKernelGGL((distill_small_kernel<TYPE, 16, FORWARD>), grid, block, 0, st, p);
 }
 
+template <int TYPE, int T, int NV>
+static void launch_chunks(const DistillParams &p, hipStream_t st) {
+    const dim3 grid(p.run * p.chunks), block(T);
+    if (p.rest) hipLaunchKernelGGL((distill_kernel<TYPE, T, NV, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((distill_kernel<TYPE, T, NV, false>), grid, block, 0, st, p);
+}
 template <int TYPE>
-static void launch_loss(const DistillParams &p, uint32_t nv, hipStream_t st) {
-    const dim3 grid(p.run * p.chunks), block(THREADS);
-    if (p.rest && nv == 2) hipLaunchKernelGGL((distill_kernel<TYPE, 2, true>), grid, block, 0, st, p);
-    else if (p.rest) hipLaunchKernelGGL((distill_kernel<TYPE, 8, true>), grid, block, 0, st, p);
-    else if (nv == 2) hipLaunchKernelGGL((distill_kernel<TYPE, 2, false>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((distill_kernel<TYPE, 8, false>), grid, block, 0, st, p);
+static void launch_loss(const DistillParams &p, Way way, uint32_t nv, hipStream_t st) {
+    if (way == Way::wave) launch_chunks<TYPE, 64, 4>(p, st);
+    else if (nv == 2) launch_chunks<TYPE, THREADS, 2>(p, st);
+    else launch_chunks<TYPE, THREADS, 8>(p, st);
     if (p.chunks > 1) hipLaunchKernelGGL((distill_join_kernel<TYPE>), dim3(p.run), dim3(64), 0, st, p);
 }
 
@@ -512,47 +526,54 @@ static void launch_in_one(DistillParams &p, hipStream_t st) {
     const uint32_t vecs = vecs_of(TYPE, p.l.classes);
     p.chunks = 1;
     p.chunk_vecs = vecs;
-    if (vecs <= 2 * THREADS) launch_row_kernel<TYPE, THREADS, 2>(p, st);
+    if (vecs <= WAVE_VECS) launch_row_kernel<TYPE, 64, 4>(p, st);
+    else if (vecs <= 2 * THREADS) launch_row_kernel<TYPE, THREADS, 2>(p, st);
     else if (vecs <= 8 * THREADS) launch_row_kernel<TYPE, THREADS, 8>(p, st);
     else if (vecs <= 16 * THREADS) launch_row_kernel<TYPE, THREADS, 16>(p, st);
     else if (vecs <= 16 * 512) launch_row_kernel<TYPE, 512, 16>(p, st);
     else launch_row_kernel<TYPE, 1024, 16>(p, st);
 }
 
-static void launch_gradient(const DistillParams &p, uint32_t nv, hipStream_t st) {
-#define CALL(T) if (nv == 0) launch_small<T, false>(p, st); else hipLaunchKernelGGL((distill_grad_kernel<T, 4>), dim3(p.run * p.chunks), dim3(THREADS), 0, st, p)
-    ISR_BY_TYPE(p.l.type, CALL)
-#undef CALL
+template <int TYPE>
+static void launch_gradient(const DistillParams &p, Way way, hipStream_t st) {
+    const dim3 grid(p.run * p.chunks);
+    if (way == Way::sixteen) launch_small<TYPE, false>(p, st);
+    else if (way == Way::wave) hipLaunchKernelGGL((distill_grad_kernel<TYPE, 64, 4>), grid, dim3(64), 0, st, p);
+    else hipLaunchKernelGGL((distill_grad_kernel<TYPE, THREADS, 4>), grid, dim3(THREADS), 0, st, p);
 }
 
 hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st) {
-    const bool in_one = p.grad && distill_in_one(p.l.type, p.l.classes, p.top);
-    const RowCut gradient = cut_gradient(p.l, cut.nv == 0);
+    const bool in_one = p.grad && distill_in_one(p.l.type, p.l.classes);
+    const RowCut gradient = cut_gradient(p.l);
     p.parts = (Part *)workspace;
     return by_runs(p, cut.rows, [&](uint32_t rows) {
         p.run = rows;
         p.chunks = cut.chunks;
         p.chunk_vecs = cut.chunk_vecs;
 #define CALL(T)                                                                          \
-    if (cut.nv == 0) launch_small<T, true>(p, st);                                       \
+    if (cut.way == Way::sixteen) launch_small<T, true>(p, st);                           \
     else if (in_one) launch_in_one<T>(p, st);                                            \
-    else launch_loss<T>(p, cut.nv, st)
+    else launch_loss<T>(p, cut.way, cut.nv, st)
         ISR_BY_TYPE(p.l.type, CALL)
 #undef CALL
         if (!p.grad || in_one) return;
         p.chunks = gradient.chunks;
         p.chunk_vecs = gradient.chunk_vecs;
-        launch_gradient(p, gradient.nv, st);
+#define CALL(T) launch_gradient<T>(p, gradient.way, st)
+        ISR_BY_TYPE(p.l.type, CALL)
+#undef CALL
     });
 }
 
 hipError_t launch_distill_grad(DistillParams p, hipStream_t st) {
-    const RowCut cut = cut_gradient(p.l, small(p.l.classes, p.top));
+    const RowCut cut = cut_gradient(p.l);
     p.chunks = cut.chunks;
     p.chunk_vecs = cut.chunk_vecs;
     return by_runs(p, cut.rows, [&](uint32_t rows) {
         p.run = rows;
-        launch_gradient(p, cut.nv, st);
+#define CALL(T) launch_gradient<T>(p, cut.way, st)
+        ISR_BY_TYPE(p.l.type, CALL)
+#undef CALL
     });
 }
 

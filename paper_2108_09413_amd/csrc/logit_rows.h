@@ -12,19 +12,26 @@ struct LogitRows {
     float scale;
 };
 
-// How rows are cut into chunks of a workgroup each, and what the chunks need of the workspace.
+// How rows go, and how they are cut into chunks of a workgroup each and what those need of the workspace.
+enum class Way {
+    sixteen,   // 16 lanes a row
+    wave,      // a wave a row
+    chunks,    // a workgroup a chunk
+    row        // a workgroup a row, chunk by chunk
+};
+constexpr uint32_t WAVE_VECS = 256;   // of a row that a wave holds by vectors
 struct RowCut {
-    uint32_t nv;           // vectors of 16 bytes a thread; 0: 16 lanes a row
+    Way way;
+    uint32_t nv;           // vectors of 16 bytes a thread of a chunk
     uint32_t chunks;       // of a row
     uint32_t chunk_vecs;   // vectors of a chunk, the last one's may be fewer
     uint32_t list_cap;     // room for candidates of the top alternatives, of a chunk
     uint32_t rows;         // of a launch
-    bool whole;            // a workgroup goes through all chunks of a row
     size_t parts_bytes, lists_bytes;
 };
-bool small_rows(uint32_t classes, uint32_t serial);
-RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, bool small);
-RowCut cut_gradient(const LogitRows &l, bool small);
+RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top);
+RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top);
+RowCut cut_gradient(const LogitRows &l);
 
 struct Part;
 // row0 to lists: set by the launcher, for each launch
@@ -38,7 +45,6 @@ struct LogprobsParams {
     uint64_t row0;
     uint32_t run;             // rows
     uint32_t chunks, chunk_vecs, list_cap;
-    bool whole;
     Part *parts;
     uint2 *lists;
 };
@@ -81,13 +87,11 @@ struct DistillParams {
     Part *parts;
 };
 
-RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top);
 hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st);
 hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st);
 
 // Whether loss and gradient of rows of this shape are one launch, which needs neither a workspace nor the statistics.
-bool distill_in_one(int type, uint32_t classes, uint32_t top);
-RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top);
+bool distill_in_one(int type, uint32_t classes);
 hipError_t launch_distill(DistillParams p, const RowCut &cut, void *workspace, hipStream_t st);   // the gradient too, if p.grad
 hipError_t launch_distill_grad(DistillParams p, hipStream_t st);
 

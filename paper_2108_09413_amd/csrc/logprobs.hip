@@ -8,7 +8,8 @@
 // the chunks and 6.0 for the join.
 // Gradient: element by element from the row's statistics, bound by memory too: 2048 x 65537 bf16 in 97 us, 5.5 TB/s; the few
 // named classes are stored behind the others.
-// Rows of up to 256 classes go by 16 lanes each.
+// Rows of up to 256 classes go by 16 lanes each, 100000 x 256 bf16 with entropy in 13 us (4.0 TB/s); of up to 1024 by a wave
+// each, 100000 x 1000 bf16 in 48 (4.2 TB/s).
 #include <algorithm>
 
 #include "logit_device.h"
@@ -540,13 +541,13 @@ __device__ __forceinline__ Slope<Val, ENT> row_slope(const LogprobsGradParams &p
             -p.l.scale * uh * LN2, !(counted || uh != 0.f) || logs == NEG_INF};
 }
 
-template <int TYPE, int NV, bool ENT>
-__global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(const LogprobsGradParams p) {
+template <int TYPE, int T, int NV, bool ENT>
+__global__ __launch_bounds__(T) void logprobs_grad_kernel(const LogprobsGradParams p) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     const uint32_t row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks, lane = threadIdx.x & 63;
     const uint64_t r = p.row0 + row;
-    const Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+    const Chunk<TYPE, T, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
     Named named;
     named.load(p.given + r * p.n_given, p.n_given);
     float u[2];
@@ -652,48 +653,220 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_small_kernel(const Logp
         if (lane + 16 * i < n) out[lane + 16 * i] = K::grad(f.zero ? 0.f : f(K::val(raw[i])) + p.l.scale * named[i]);
 }
 
-// ---- launches --------------------------------------------------------------------------------
+// ---- rows of up to 1024 classes: a wave a row, E elements a lane ----------------------------
 
-// 16 lanes a row where what they do one after the other (`serial` steps, each over a lane's elements) stays short; always
-// below 16 classes, where a vector of 16 bytes may not fit.
-bool small_rows(uint32_t classes, uint32_t serial) {
-    return classes < 16 || (classes <= 256 && serial * ((classes + 15) / 16) <= 256);
+// A bound that k of the lanes' largest reach lets few elements more through.  Where it lets too many, and for many alternatives, the
+// bound is searched among all elements: exactly k reach it, or those equal to it are taken by ascending class.
+template <int TYPE, int E, bool TOP, bool ENT>
+__global__ __launch_bounds__(THREADS) void logprobs_wave_kernel(const LogprobsParams p) {
+    using K = Kind<TYPE>;
+    using Val = typename K::Val;
+    __shared__ __attribute__((aligned(16))) uint2 lists[TOP ? THREADS / 64 : 1][ISR_MAX_TOP];
+    const uint32_t lane = threadIdx.x & 63, row = blockIdx.x * (THREADS / 64) + (threadIdx.x >> 6), n = p.l.classes;
+    if (row >= p.run) return;   // the whole wave
+    const uint64_t r = p.row0 + row;
+    const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
+    typename K::Raw raw[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) raw[i] = x[min(lane + 64 * i, n - 1)];
+    auto has = [&](int i) { return lane + 64 * i < n; };
+    int32_t c[2];
+    Val at[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t g = lane + 64 * h;
+        c[h] = g < p.n_given ? p.given[r * p.n_given + g] : -1;
+        at[h] = (uint32_t)c[h] < n ? K::val(x[c[h]]) : lowest(Val());
+    }
+    Stat<Val> a{lowest(Val()), 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (has(i)) a.m = larger(a.m, K::val(raw[i]));
+    a.m = wave_max(a.m);
+    const float scale = p.l.scale * LOG2E;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        if (!has(i)) continue;
+        const float d = scale * below(K::val(raw[i]), a.m), e = __builtin_amdgcn_exp2f(d);
+        a.s += e;
+        if (ENT) a.t += e * fmaxf(d, NO_SHARE);
+    }
+    a.s = wave_sum(a.s);
+    if (ENT) a.t = wave_sum(a.t);
+    const Logp<Val> logp(p.l, a);
+    const float nan = __builtin_nanf("");
+    if (lane == 0) {
+        if (ENT) p.entropy[r] = logp.bad ? nan : logp.empty ? 0.f : logp.logs - LN2 * (a.t / a.s);
+        if (p.stats) { p.stats[2 * r] = bits_of(a.m); p.stats[2 * r + 1] = logp.bad ? nan : logp.empty ? NEG_INF : logp.logs; }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t g = lane + 64 * h;
+        if (g < p.n_given) p.logprob[r * p.n_given + g] = c[h] < 0 ? 0.f : (uint32_t)c[h] < n ? logp(at[h]) : nan;
+    }
+    if constexpr (TOP) {
+        uint32_t key[E], valid = 0, least = ~0u;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const Val v = K::val(raw[i]);
+            const bool is = has(i) && possible(v) && !logp.bad;
+            key[i] = is ? key_of(v) : 0;
+            valid |= (uint32_t)is << i;
+            least = min(least, is ? key[i] : ~0u);
+        }
+        const uint32_t most = key_of(a.m);
+        least = min(wave_fold(least, [](uint32_t u, uint32_t v) { return min(u, v); }), most);
+        auto count = [&](auto test) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) m += __popcll(__ballot((valid >> i & 1) && test(key[i])));
+            return m;
+        };
+        const uint32_t all = count([](uint32_t) { return true; }), k = min(p.top, all);
+        // listed are `more` elements above the bound, and as many that are equal to it, by class, as make `total`
+        uint32_t bound = 0, more = k, total = k;
+        // us of 100000 rows by the lanes' bound / exactly: 256 classes f32 with 48 147 / 156, 56: 172 / 157; 1000 classes 220 / 282, 273 / 286
+        bool exactly = k > 48 && all > k;
+        if (all > k) {
+            uint32_t own = 0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) own = max(own, key[i]);
+            const int top = 31 - __builtin_clz((least ^ most) | 1);
+            const uint32_t prefix = (most >> top >> 1) << top << 1;
+            if (!exactly) {
+                bound = prefix;
+                uint32_t reached = 64;
+                for (int b = top; b >= LOW_BITS<TYPE> && reached != k; --b) {
+                    const uint32_t next = bound | (1u << b), m = (uint32_t)__popcll(__ballot(own >= next));
+                    if (m >= k) { bound = next; reached = m; }
+                }
+                more = total = count([&](uint32_t u) { return u >= bound; });
+                bound -= 1;   // from 0 on all reach it
+                exactly = total > ISR_MAX_TOP;
+            }
+            if (exactly) {
+                bound = prefix;
+                total = k;
+                uint32_t reached = all;
+                for (int b = top; b >= LOW_BITS<TYPE> && reached != k; --b) {
+                    const uint32_t next = bound | (1u << b), m = count([&](uint32_t u) { return u >= next; });
+                    if (m >= k) { bound = next; reached = m; }
+                }
+                if (reached == k) {
+                    more = k;
+                    bound -= 1;
+                } else {
+                    if (LOW_BITS<TYPE>) bound |= bound >> 31 ? 0 : (1u << LOW_BITS<TYPE>) - 1;   // the bits that all 16-bit logits have there
+                    more = count([&](uint32_t u) { return u > bound; });
+                }
+            }
+        }
+        const bool whole = total == all;
+        uint2 *const list = lists[threadIdx.x >> 6];
+        uint32_t above = 0, equal = more;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const bool is = valid >> i & 1, up = is && (whole || key[i] > bound), even = is && !up && key[i] == bound;
+            const uint64_t ups = __ballot(up), evens = __ballot(even);
+            const uint32_t place = up ? above + lanes_before(ups) : equal + lanes_before(evens);
+            if ((up || even) && place < total) list[place] = make_uint2(key[i], ~(lane + 64 * i));
+            above += __popcll(ups);
+            equal += __popcll(evens);
+        }
+        wave_order();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t i = lane + 64 * h;
+            if (i < total) {
+                const uint2 mine = list[i];
+                const uint64_t own = (uint64_t)mine.x << 32 | mine.y;
+                uint32_t place = 0;
+                for (uint32_t j = 0; j < total; ++j) place += ((uint64_t)list[j].x << 32 | list[j].y) > own;
+                if (place < k) {
+                    p.top_class[r * p.top + place] = (int32_t)~mine.y;
+                    p.top_logprob[r * p.top + place] = logp(of_key<Val>(mine.x));
+                }
+            }
+            if (i >= k && i < p.top) {
+                p.top_class[r * p.top + i] = -1;
+                p.top_logprob[r * p.top + i] = logp.bad ? nan : NEG_INF;
+            }
+        }
+    }
 }
 
-RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, bool small) {
+// ---- launches --------------------------------------------------------------------------------
+
+// 16 lanes a row, of up to 16 elements each, where what they do one after the other (`serial` steps, each over a lane's elements) stays
+// below `most`; always below 16 classes, where a vector of 16 bytes may not fit.  100000 rows of f32, us by 16 lanes / by a wave:
+// 256 classes with entropy 17 / 29, with 10 alternatives 71 / 87, 16: 103 / 90; 64 classes with 40: 95 / 96, 48: 112 / 100; loss of
+// 256 classes and 16 entries 72 / 92, 64 and 64: 72 / 94, 17 and 128: 128 / 107.
+constexpr uint32_t SMALL = 256;   // classes
+static bool sixteen_lanes(uint32_t classes, uint32_t serial, uint32_t most) {
+    return classes < 16 || (classes <= SMALL && serial * ((classes + 15) / 16) <= most);
+}
+
+static uint32_t vecs_of(int type, uint32_t classes) { return classes / (type == ISR_F32 || type == ISR_I32 ? 4 : 8); }
+constexpr uint32_t MOST_GROUPS = 1u << 22;   // of a launch
+
+// Rows whose workgroup (or its share) does them in one go, `groups` rows a workgroup.
+static RowCut whole_rows(Way way, int type, uint32_t classes, uint64_t rows, uint32_t groups) {
     RowCut cut{};
-    const uint32_t vecs = classes / (type == ISR_F32 || type == ISR_I32 ? 4 : 8);
-    const uint32_t most = 1u << 22;   // workgroups of a launch
-    if (small) {
-        cut.rows = (uint32_t)std::min<uint64_t>(rows, (uint64_t)most * (THREADS / 16));
-        cut.chunks = 1;
-        return cut;
-    }
+    cut.way = way;
+    cut.chunks = 1;
+    cut.chunk_vecs = vecs_of(type, classes);
+    cut.rows = (uint32_t)std::min<uint64_t>(rows, (uint64_t)MOST_GROUPS * groups);
+    return cut;
+}
+
+RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top) {
+    RowCut cut{};
+    const uint32_t vecs = vecs_of(type, classes);
     auto chunks_of = [&](uint32_t nv) { return (vecs + nv * THREADS - 1) / (nv * THREADS); };
+    cut.way = Way::chunks;
     // Few rows: smaller chunks on more CUs, as long as the join still reads their lists at once
     cut.nv = vecs <= 2 * THREADS ? 2 : vecs > 8 * THREADS && rows * chunks_of(8) <= 512 && chunks_of(4) <= 16 && top ? 4 : 8;
     cut.chunks = chunks_of(cut.nv);
     cut.chunk_vecs = (vecs + cut.chunks - 1) / cut.chunks;
     cut.chunks = (vecs + cut.chunk_vecs - 1) / cut.chunk_vecs;   // none of them empty
-    cut.whole = top && cut.chunks > 1 && rows >= WHOLE_ROWS && (top <= WHOLE_TOP || cut.chunks <= WHOLE_CHUNKS);
+    if (top && cut.chunks > 1 && rows >= WHOLE_ROWS && (top <= WHOLE_TOP || cut.chunks <= WHOLE_CHUNKS)) cut.way = Way::row;
     cut.list_cap = cut.chunks == 1 ? LIST : std::max(128u, 2 * top + 64);
-    cut.rows = (uint32_t)std::min<uint64_t>(rows, std::max<uint32_t>(1, most / cut.chunks));
-    if (cut.whole) return cut;
-    cut.parts_bytes = cut.chunks == 1 ? 0 : ((size_t)cut.rows * cut.chunks * sizeof(Part) + 255) / 256 * 256;
-    cut.lists_bytes = cut.chunks == 1 || !top ? 0 : (size_t)cut.rows * cut.chunks * cut.list_cap * sizeof(uint2);
+    cut.rows = (uint32_t)std::min<uint64_t>(rows, std::max<uint32_t>(1, MOST_GROUPS / cut.chunks));
+    if (cut.way == Way::row || cut.chunks == 1) return cut;
+    cut.parts_bytes = ((size_t)cut.rows * cut.chunks * sizeof(Part) + 255) / 256 * 256;
+    cut.lists_bytes = top ? (size_t)cut.rows * cut.chunks * cut.list_cap * sizeof(uint2) : 0;
     return cut;
 }
 
-RowCut cut_gradient(const LogitRows &l, bool small) {
-    if (small) return cut_rows(l.type, l.classes, l.rows, 0, true);
+RowCut cut_gradient(const LogitRows &l) {
+    // 100000 rows of f32 by 16 lanes / by a wave, us: 256 classes with 1 named 33 / 40, 32: 75 / 111, 128: 305 / 340, 17 with 128: 162 / 336
+    if (l.classes <= SMALL) return whole_rows(Way::sixteen, l.type, l.classes, l.rows, THREADS / 16);
+    const uint32_t vecs = vecs_of(l.type, l.classes);
+    // 100000 rows, four waves a row / one, us: 257 f32 127 / 44, 1000 f32 202 / 153, 1000 bf16 187 / 79
+    if (vecs <= WAVE_VECS) return whole_rows(Way::wave, l.type, l.classes, l.rows, 1);
     RowCut cut{};
-    const uint32_t vecs = l.classes / (l.type == ISR_F32 || l.type == ISR_I32 ? 4 : 8);
+    cut.way = Way::chunks;
     cut.nv = 4;   // nothing is exchanged between threads but the named classes: smaller chunks, more of them
     cut.chunks = (vecs + 4 * THREADS - 1) / (4 * THREADS);
     cut.chunk_vecs = (vecs + cut.chunks - 1) / cut.chunks;
     cut.chunks = (vecs + cut.chunk_vecs - 1) / cut.chunk_vecs;
-    cut.rows = (uint32_t)std::min<uint64_t>(l.rows, std::max<uint32_t>(1, (1u << 22) / cut.chunks));
+    cut.rows = (uint32_t)std::min<uint64_t>(l.rows, std::max<uint32_t>(1, MOST_GROUPS / cut.chunks));
     return cut;
+}
+
+RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top) {
+    if (sixteen_lanes(classes, top, 176)) return whole_rows(Way::sixteen, type, classes, rows, THREADS / 16);
+    // 16 elements a lane at most.  100000 rows by a workgroup / by a wave, us: 257 f32 with entropy 98 / 30, with 5 alternatives
+    // 267 / 85; 1024 f32 125 / 71, 273 / 148; 1024 bf16 111 / 49, 271 / 146
+    if (classes <= 1024) return whole_rows(Way::wave, type, classes, rows, THREADS / 64);
+    return cut_rows(type, classes, rows, top);
+}
+
+RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top) {
+    if (sixteen_lanes(classes, top, 256)) return whole_rows(Way::sixteen, type, classes, rows, THREADS / 16);
+    // 100000 rows by four waves / by one, loss / with gradient, us: 257 f32 140, 193 / 90, 100; 1000 bf16 172, 254 / 114, 152
+    if (vecs_of(type, classes) <= WAVE_VECS) return whole_rows(Way::wave, type, classes, rows, 1);
+    return cut_rows(type, classes, rows, 0);
 }
 
 template <int TYPE, int NV>
@@ -725,11 +898,21 @@ static void launch_small(const Params &p, hipStream_t st) {
     else launch_small<TYPE, 16>(p, st);
 }
 
+template <int TYPE, int E>
+static void launch_wave(const LogprobsParams &p, hipStream_t st) {
+    const dim3 grid((p.run + THREADS / 64 - 1) / (THREADS / 64)), block(THREADS);
+    if (p.top && p.entropy) hipLaunchKernelGGL((logprobs_wave_kernel<TYPE, E, true, true>), grid, block, 0, st, p);
+    else if (p.top) hipLaunchKernelGGL((logprobs_wave_kernel<TYPE, E, true, false>), grid, block, 0, st, p);
+    else if (p.entropy) hipLaunchKernelGGL((logprobs_wave_kernel<TYPE, E, false, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((logprobs_wave_kernel<TYPE, E, false, false>), grid, block, 0, st, p);
+}
+
 template <int TYPE>
-static void launch_rows(const LogprobsParams &p, uint32_t nv, hipStream_t st) {
-    if (nv == 0) return launch_small<TYPE>(p, st);
+static void launch_rows(const LogprobsParams &p, Way way, uint32_t nv, hipStream_t st) {
+    if (way == Way::sixteen) return launch_small<TYPE>(p, st);
+    if (way == Way::wave) return p.l.classes <= 512 ? launch_wave<TYPE, 8>(p, st) : launch_wave<TYPE, 16>(p, st);
     const dim3 grid(p.run), block(THREADS);
-    if (p.whole) {
+    if (way == Way::row) {
         if (p.entropy) hipLaunchKernelGGL((logprobs_row_top_kernel<TYPE, 8, true>), grid, block, 0, st, p);
         else hipLaunchKernelGGL((logprobs_row_top_kernel<TYPE, 8, false>), grid, block, 0, st, p);
         return;
@@ -745,38 +928,40 @@ static void launch_rows(const LogprobsParams &p, uint32_t nv, hipStream_t st) {
     else hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 0>), grid, block, 0, st, p);
 }
 
-RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top) { return cut_rows(type, classes, rows, top, small_rows(classes, top)); }
-
 hipError_t launch_logprobs(LogprobsParams p, const RowCut &cut, void *workspace, hipStream_t st) {
     p.chunks = cut.chunks;
     p.chunk_vecs = cut.chunk_vecs;
     p.list_cap = cut.list_cap;
-    p.whole = cut.whole;
     p.parts = (Part *)workspace;
     p.lists = (uint2 *)((uint8_t *)workspace + cut.parts_bytes);
     return by_runs(p, cut.rows, [&](uint32_t rows) {
         p.run = rows;
-#define CALL(T) launch_rows<T>(p, cut.nv, st)
+#define CALL(T) launch_rows<T>(p, cut.way, cut.nv, st)
         ISR_BY_TYPE(p.l.type, CALL)
 #undef CALL
     });
 }
 
+template <int TYPE, int T>
+static void launch_grad_chunks(const LogprobsGradParams &p, hipStream_t st) {
+    const dim3 grid(p.run * p.chunks), block(T);
+    if (p.up_entropy) hipLaunchKernelGGL((logprobs_grad_kernel<TYPE, T, 4, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((logprobs_grad_kernel<TYPE, T, 4, false>), grid, block, 0, st, p);
+}
 template <int TYPE>
-static void launch_grad_rows(const LogprobsGradParams &p, uint32_t nv, hipStream_t st) {
-    const dim3 grid(p.run * p.chunks), block(THREADS);
-    if (nv == 0) launch_small<TYPE>(p, st);
-    else if (p.up_entropy) hipLaunchKernelGGL((logprobs_grad_kernel<TYPE, 4, true>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((logprobs_grad_kernel<TYPE, 4, false>), grid, block, 0, st, p);
+static void launch_grad_rows(const LogprobsGradParams &p, Way way, hipStream_t st) {
+    if (way == Way::sixteen) launch_small<TYPE>(p, st);
+    else if (way == Way::wave) launch_grad_chunks<TYPE, 64>(p, st);
+    else launch_grad_chunks<TYPE, THREADS>(p, st);
 }
 
 hipError_t launch_logprobs_grad(LogprobsGradParams p, hipStream_t st) {
-    const RowCut cut = cut_gradient(p.l, small_rows(p.l.classes, p.n_given));
+    const RowCut cut = cut_gradient(p.l);
     p.chunks = cut.chunks;
     p.chunk_vecs = cut.chunk_vecs;
     return by_runs(p, cut.rows, [&](uint32_t rows) {
         p.run = rows;
-#define CALL(T) launch_grad_rows<T>(p, cut.nv, st)
+#define CALL(T) launch_grad_rows<T>(p, cut.way, st)
         ISR_BY_TYPE(p.l.type, CALL)
 #undef CALL
     });

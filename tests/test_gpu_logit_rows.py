@@ -102,7 +102,7 @@ def check_grad(isr, torch, kind, dev, wide, scale, given, up, up_h, r, out=None)
     return got
 
 
-CLASSES = [1, 2, 3, 7, 10, 16, 17, 64, 101, 255, 256, 257, 511, 1000, 2047, 2049, 4099, 8193, 16385, 32771, 50021, 131080]
+CLASSES = [1, 2, 3, 7, 10, 15, 16, 17, 64, 65, 101, 128, 129, 255, 256, 257, 511, 513, 1000, 1024, 1025, 2047, 2049, 2055, 4099, 8193, 16385, 32771, 50021, 131080]
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -122,7 +122,7 @@ def test_logprobs_and_gradient(isr, torch, kind, classes):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "i32"])
-@pytest.mark.parametrize("rows,classes,top", [(1, 10, 10), (63, 10, 2), (4099, 10, 1), (1000, 101, 5), (70, 257, 64), (300, 1000, 20), (17, 4096, 128)])
+@pytest.mark.parametrize("rows,classes,top", [(1, 10, 10), (63, 10, 2), (4099, 10, 1), (1000, 101, 5), (203, 200, 128), (70, 257, 64), (300, 1000, 20), (301, 1000, 128), (17, 4096, 128)])
 def test_many_rows(isr, torch, kind, rows, classes, top):
     rng = np.random.default_rng(rows)
     dev, wide = make(torch, kind, rows, classes, rows, pad=rows % 3)
@@ -242,7 +242,7 @@ def special_rows(kind, classes, rng):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("classes", [2, 10, 101, 256, 300, 2500, 20011, 70001])
+@pytest.mark.parametrize("classes", [2, 10, 101, 256, 300, 1000, 2500, 20011, 70001])
 def test_masked_tied_and_extreme_rows(isr, torch, kind, classes):
     rng = np.random.default_rng(classes)
     named = special_rows(kind, classes, rng)
@@ -339,7 +339,7 @@ def test_distillation_of_many_rows(isr, torch, kind, rest, rows, classes, top):
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "i32"])
 @pytest.mark.parametrize("rest", [False, True])
-@pytest.mark.parametrize("classes", [10, 101, 300, 20011])
+@pytest.mark.parametrize("classes", [10, 101, 300, 1030, 5000, 20011, 70001])
 def test_distillation_of_special_rows(isr, torch, kind, rest, classes):
     rng = np.random.default_rng(classes)
     named = special_rows(kind, classes, rng)
