@@ -236,7 +236,8 @@ int isr_logprobs(const isr_logits *logits, const int32_t *given_device, uint32_t
  * A row whose given classes are all negative and whose grad_entropy is absent or 0 gets zeros
  * whatever it holds; so does an empty row.  grad_logits_device: [rows][grad_row_stride] of the logits'
  * type (float for int32 logits), columns from `classes` on are left as they are; may be
- * the logits' own memory, with their stride, and must not overlap it otherwise. */
+ * the logits' own memory, with their stride, and otherwise lies in front of the logits' first
+ * element or behind their last (not between their rows). */
 int isr_logprobs_grad(const isr_logits *logits, const int32_t *given_device, uint32_t given,
                       const float *grad_logprob_device, const float *entropy_device,
                       const float *grad_entropy_device, const float *stats_device,
@@ -260,7 +261,7 @@ typedef struct isr_teacher {
 /* loss[r] = sum_i q_i (log q_i - log p_{c_i}) [+ q_rest (log q_rest - log p_rest), p_rest the
  * student's probability of all classes that are no entry], terms with q = 0 left out.  A row
  * without an entry (or, rest == 0, with all its values -infinity) has loss 0 and gradient 0 whatever
- * it holds.  An empty row has gradient 0.  A class named by two entries gets both their q.
+ * it holds.  An empty row has gradient 0 (NaN where the teacher's entries make the row NaN).  A class named by two entries gets both their q.
  *   row_weight_device     float [rows] or NULL (1): the gradient's factor, i.e. the gradient by
  *                         loss[r] of what is trained; 0 gives gradient 0 whatever the row holds
  *   loss_device           float [rows], without the weight

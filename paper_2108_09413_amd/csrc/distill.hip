@@ -150,7 +150,7 @@ __device__ __forceinline__ DistillStat conclude(const DistillParams &p, uint64_t
     }
     const bool bad = t.bad || all.s != all.s;
     if (writes) p.loss[r] = bad ? __builtin_nanf("") : (float)loss;
-    return DistillStat{bits_of(all.m), empty ? NEG_INF : logs, bits_of(a.m), rest_logs, t.value_m, t.value_logs, bad ? __builtin_nanf("") : (float)t.total, (float)t.left};
+    return DistillStat{bits_of(all.m), empty && !bad ? NEG_INF : logs, bits_of(a.m), rest_logs, t.value_m, t.value_logs, bad ? __builtin_nanf("") : (float)t.total, (float)t.left};
 }
 
 // ---- gradient ---------------------------------------------------------------------------------
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
             loss += left * (logf((float)left) - lr);
         }
         const bool nan = bad || all.s != all.s;
-        st = DistillStat{bits_of(all.m), empty ? NEG_INF : logs, bits_of(a.m), rest_logs, value_m, value_logs,
+        st = DistillStat{bits_of(all.m), empty && !nan ? NEG_INF : logs, bits_of(a.m), rest_logs, value_m, value_logs,
                          nan ? __builtin_nanf("") : (float)total, (float)left};
         if (none) st = DistillStat{0.f, NEG_INF, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (store && lane == 0) {

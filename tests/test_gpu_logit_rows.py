@@ -379,6 +379,38 @@ def test_special_teachers(isr, torch, rest):
         check_distill(isr, torch, kind, dev, wide, 1.0, teacher, 1.0, rest, rng.normal(size=8), in_place=True)
 
 
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("classes", [6, 40, 300, 5000])
+def test_bad_teachers_of_empty_rows(isr, torch, rest, classes):
+    """A class outside or a NaN value makes all of a row's results NaN, of an empty row too; a weight of 0 its gradient 0."""
+    entry = np.tile(np.arange(3), (5, 1))
+    entry[0, 1] = classes
+    value = np.log(np.tile([0.1, 0.2, 0.3], (5, 1)))
+    value[1, 2] = np.nan
+    value[3, 0] = np.nan
+    dev, wide = put(torch, "f32", np.full((5, classes), -np.inf))
+    teacher = (entry, torch.from_numpy(value).float().double().numpy(), torch.from_numpy(entry.astype(np.int32)).cuda(), torch.from_numpy(value).float().cuda())
+    check_distill(isr, torch, "f32", dev, wide, 1.0, teacher, 1.0, rest, np.array([1.0, -2.0, 1.0, 0.0, 3.0]), in_place=True)
+
+
+def test_more_rows_of_one_wave_or_workgroup_than_a_launch_takes(isr, torch):
+    """As above, for log-probabilities by a wave and by a workgroup a row."""
+    for classes, rows, top in ((257, (1 << 24) + 5, 1), (1025, (1 << 22) + 5, 2)):
+        print(classes, rows, flush=True)
+        x = torch.empty((rows, classes), device="cuda", dtype=torch.bfloat16).uniform_(-4, 0)
+        x[:, 0] = 1
+        x[:, 1] = 2
+        g = torch.ones((rows, 1), device="cuda", dtype=torch.int32)
+        at = torch.tensor([0, 1, (1 << 22) - 1, 1 << 22, (1 << 22) + 1, rows - 6, rows - 5, rows - 2, rows - 1])
+        few = x[at].contiguous()
+        r, s = (isr.isr_logprobs(z, g[:len(z)], top=top, entropy=True, stats=True) for z in (x, few))
+        _, h, tc, tl = plain.logprobs(few.double().cpu().numpy(), 1.0, None, top)
+        for q, of in ((r, at), (s, slice(None))):
+            assert np.array_equal(q.top_class[of].cpu().numpy(), tc)
+            close(q.top[of], tl, plain.logp_tol(tl), "top log-probabilities")
+            close(q.entropy[of], h, plain.U * plain.SUM * (3 + 2 * math.log(classes)), "entropy")
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 def test_gradient_over_the_logits_and_foreign_memory(isr, torch, kind):
     """In place, with foreign columns; and into rows of another stride: what lies between and behind the rows stays."""
