@@ -1,7 +1,7 @@
 // Distillation from a teacher's top logits: the loss of each row and its gradient.
 //
 // Loss alone: chunks of a row in registers, one workgroup each, and a join, as for the log-probabilities; with a rest class the
-// entries are left out of the chunks' sums.  Gradient alone: by elements from the row's statistics.
+// entries are left out of the chunks' sums; of few rows 1024 threads hold up to 8192 vectors, and no join follows.  Gradient alone: by elements from the row's statistics.
 // Both at once, rows that fit the registers of a workgroup (up to 16384 vectors of 16 bytes): the row is read once, held, and
 // its gradient stored from there, 4096 x 131072 bf16 with 64 entries and rest in 434 us (4.95 TB/s, of 5.8 that the
 // gradient alone reaches), 8192 x 32000 in 199 (5.3).  Longer rows take the two ways one after the other.
@@ -275,17 +275,20 @@ __global__ __launch_bounds__(T) void distill_kernel(const DistillParams p) {
     const uint64_t r = p.row0 + row;
     // in front of the row's loads, behind which it would have to wait for them
     const RowEntries<T> entries(p, r);
+    const bool whole = p.chunks == 1;
+    Entries<TYPE> e;
+    if (whole && tid < 64) e.load(p, r);
     Chunk<TYPE, T, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+    Taught t;
+    if (whole && tid < 64) t = taught<TYPE>(p, e, table);   // while the row arrives
     const float c = p.l.scale * LOG2E;
     const Stat<Val> all = block_stat<T, false>(chunk_stat<REST>(k, p.l.classes, c, entries, mask), c, sh, [] {});
-    if (p.chunks > 1) {
+    if (!whole) {
         if (tid == 0) p.parts[(size_t)row * p.chunks + chunk] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, 0.f, 0};
         return;
     }
     if (tid >= 64) return;
-    Entries<TYPE> e;
-    e.load(p, r);
-    const DistillStat st = conclude<TYPE>(p, r, all, e, taught<TYPE>(p, e, table));
+    const DistillStat st = conclude<TYPE>(p, r, all, e, t);
     if (p.stats && tid == 0) p.stats[r] = st;
 }
 
@@ -514,6 +517,8 @@ static void launch_chunks(const DistillParams &p, hipStream_t st) {
 template <int TYPE>
 static void launch_loss(const DistillParams &p, Way way, uint32_t nv, hipStream_t st) {
     if (way == Way::wave) launch_chunks<TYPE, 64, 4>(p, st);
+    else if (way == Way::alone && nv == 4) launch_chunks<TYPE, ALONE, 4>(p, st);
+    else if (way == Way::alone) launch_chunks<TYPE, ALONE, 8>(p, st);
     else if (nv == 2) launch_chunks<TYPE, THREADS, 2>(p, st);
     else launch_chunks<TYPE, THREADS, 8>(p, st);
     if (p.chunks > 1) hipLaunchKernelGGL((distill_join_kernel<TYPE>), dim3(p.run), dim3(64), 0, st, p);

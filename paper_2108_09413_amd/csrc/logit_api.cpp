@@ -124,7 +124,7 @@ int isr_logprobs_grad(const isr_logits *l, const int32_t *given_device, uint32_t
 // What the chunks of rows leave and, for a gradient behind them, the rows' statistics where the caller keeps none.
 size_t isr_distill_workspace_bytes(const isr_logits *l, const isr_teacher *t) {
     if (!valid_shape(l) || !valid_teacher(t) || l->rows == 0) return 0;
-    return cut_distill(l->type, l->classes, l->rows, t->top).parts_bytes + (distill_in_one(l->type, l->classes) ? 0 : l->rows * sizeof(DistillStat));
+    return cut_distill(l->type, l->classes, l->rows, t->top, t->rest != 0).parts_bytes + (distill_in_one(l->type, l->classes) ? 0 : l->rows * sizeof(DistillStat));
 }
 
 int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weight_device, float *loss_device, float *stats_device,
@@ -136,7 +136,7 @@ int isr_distill(const isr_logits *l, const isr_teacher *t, const float *row_weig
     const size_t need = isr_distill_workspace_bytes(l, t);
     if (need && (!workspace_device || workspace_bytes < need)) return ISR_ERR_WORKSPACE;
     if (need && !aligned(workspace_device, 16)) return ISR_ERR_ARG;
-    const RowCut cut = cut_distill(l->type, l->classes, l->rows, t->top);
+    const RowCut cut = cut_distill(l->type, l->classes, l->rows, t->top, t->rest != 0);
     void *stats = stats_device;
     if (!stats && grad_logits_device && !distill_in_one(l->type, l->classes)) stats = (uint8_t *)workspace_device + cut.parts_bytes;
     const DistillParams p = distill_params(l, t, row_weight_device, loss_device, stats, grad_logits_device, grad_row_stride);

@@ -17,9 +17,11 @@ enum class Way {
     sixteen,   // 16 lanes a row
     wave,      // a wave a row
     chunks,    // a workgroup a chunk
-    row        // a workgroup a row, chunk by chunk
+    row,       // a workgroup a row, chunk by chunk
+    alone      // a workgroup of ALONE threads a row
 };
 constexpr uint32_t WAVE_VECS = 256;   // of a row that a wave holds by vectors
+constexpr int ALONE = 1024;
 struct RowCut {
     Way way;
     uint32_t nv;           // vectors of 16 bytes a thread of a chunk
@@ -30,7 +32,7 @@ struct RowCut {
     size_t parts_bytes, lists_bytes;
 };
 RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top);
-RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top);
+RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top, bool rest);
 RowCut cut_gradient(const LogitRows &l);
 
 struct Part;

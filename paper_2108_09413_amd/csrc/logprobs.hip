@@ -2,10 +2,10 @@
 //
 // Forward: a row is cut into chunks of up to 256 * NV vectors of 16 bytes, one workgroup each, which holds its chunk in
 // registers: one pass over memory, then maximum, exponentials and candidates of the top alternatives from registers.  The
-// chunks' results meet in a second launch (join), or in the same one where a row is one chunk; of many rows with top
-// alternatives a workgroup goes through all chunks of one.  Bound by memory: 4096 rows of 131072 bf16 in 182 us, 5.9 TB/s,
-// with 20 alternatives in 197.  Few rows are bound by latency: one row of 131072 with 20 alternatives takes 6.8 us for
-// the chunks and 6.0 for the join.
+// chunks' results meet in a second launch (join), or in the same one where a row is one chunk: up to 2048 vectors, of few rows up
+// to 8192 by 1024 threads.  Of many rows with top alternatives a workgroup goes through all chunks of one.  Bound by memory: 4096 rows
+// of 131072 bf16 in 182 us, 5.9 TB/s, with 20 alternatives in 197.  Few rows are bound by latency: one row of 32000 bf16 with 20
+// alternatives and entropy takes 8.2 us, one of 131072 11.8 in two launches.
 // Gradient: element by element from the row's statistics, bound by memory too: 2048 x 65537 bf16 in 97 us, 5.5 TB/s; the few
 // named classes are stored behind the others.
 // Rows of up to 256 classes go by 16 lanes each, 100000 x 256 bf16 with entropy in 13 us (4.0 TB/s); of up to 1024 by a wave
@@ -17,10 +17,11 @@
 namespace isr {
 
 constexpr int LIST = 512;   // candidates of the top alternatives in LDS
-struct Shared : SharedStat<THREADS> {
+constexpr int KEYS = 256;
+struct Shared {
     uint32_t listed;
-    int count[THREADS / 64];
-    alignas(16) uint32_t key[THREADS];   // largest key of each thread
+    int count[16];   // of each wave
+    alignas(16) uint32_t key[KEYS];   // largest key of each thread, or of neighbours together
     alignas(16) uint2 list[LIST + 2];    // candidates: (key, ~class), so that the larger 64-bit number comes first
 };
 
@@ -56,7 +57,7 @@ __device__ __forceinline__ uint32_t key_bound(const Shared &sh, uint32_t k) {
     const uint32_t low = k <= 32 ? four : k <= 64 ? min(two[0], two[1]) : min(min(q.x, q.y), min(q.z, q.w));
     const uint32_t least = wave_fold(low, fold_min), most = wave_fold(four, fold_max);
     const int top = 31 - __builtin_clz((least ^ most) | 1);   // the highest bit in which two of them differ
-    uint32_t bound = (most >> top >> 1) << top << 1, reached = THREADS;
+    uint32_t bound = (most >> top >> 1) << top << 1, reached = KEYS;
     auto search = [&](int from, int to) {
         for (int b = from; b >= to; --b) {
             const uint32_t next = bound | (1u << b);
@@ -70,11 +71,14 @@ __device__ __forceinline__ uint32_t key_bound(const Shared &sh, uint32_t k) {
     return (bound >> LOW) << LOW;
 }
 
+template <int T>
 __device__ __forceinline__ int block_count(int n, Shared &sh) {
     n = wave_sum(n);
     if ((threadIdx.x & 63) == 0) sh.count[threadIdx.x >> 6] = n;
     __syncthreads();
-    n = (sh.count[0] + sh.count[1]) + (sh.count[2] + sh.count[3]);
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) n += sh.count[w];
     __syncthreads();
     return n;
 }
@@ -82,7 +86,7 @@ __device__ __forceinline__ int block_count(int n, Shared &sh) {
 // each(f): f(key, class) for the thread's own possible elements, of which all threads together have more than k.  Lists
 // exactly k: the bound is a number of 56 bits, key and ~class (below 2^24), found bit by bit.  Returns with the list complete for
 // all threads.  Rows of equal logits come here, 2048 x 65536 bf16 with 20 alternatives 2.0 ms where other rows take 0.06.
-template <class Each>
+template <int T, class Each>
 __device__ void list_exactly(Each each, uint32_t k, Shared &sh) {
     uint64_t bound = 0;
     auto number = [](uint32_t key, uint32_t cls) { return (uint64_t)key << 24 | (~cls & 0xFFFFFF); };
@@ -90,7 +94,7 @@ __device__ void list_exactly(Each each, uint32_t k, Shared &sh) {
         const uint64_t next = bound | (1ull << b);
         int n = 0;
         each([&](uint32_t key, uint32_t cls) { n += number(key, cls) >= next; });
-        n = block_count(n, sh);
+        n = block_count<T>(n, sh);
         if ((uint32_t)n >= k) bound = next;
         if ((uint32_t)n == k) break;
     }
@@ -147,12 +151,12 @@ __device__ __forceinline__ void finish_values(const LogprobsParams &p, uint64_t 
 }
 
 // The list is complete.
-template <int TYPE>
+template <int TYPE, int T>
 __device__ __forceinline__ void finish_top(const LogprobsParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a, const Shared &sh) {
     using Val = typename Kind<TYPE>::Val;
     const Logp<Val> logp(p.l, a);
     const uint32_t n = logp.bad ? 0 : min(sh.listed, (uint32_t)LIST);
-    for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
+    for (uint32_t i = threadIdx.x; i < n; i += T) {
         const uint2 mine = sh.list[i];
         const uint64_t own = (uint64_t)mine.x << 32 | mine.y;
         uint32_t place = 0;
@@ -166,7 +170,7 @@ __device__ __forceinline__ void finish_top(const LogprobsParams &p, uint64_t r, 
             p.top_logprob[r * p.top + place] = logp(of_key<Val>(mine.x));
         }
     }
-    for (uint32_t k = n + threadIdx.x; k < p.top; k += THREADS) {
+    for (uint32_t k = n + threadIdx.x; k < p.top; k += T) {
         p.top_class[r * p.top + k] = -1;
         p.top_logprob[r * p.top + k] = logp.bad ? __builtin_nanf("") : NEG_INF;
     }
@@ -199,8 +203,8 @@ struct SharedVecs {
 struct Nothing {};
 
 // The chunk's vectors that reach the bound (few; NaN does, all results of its row are NaN).
-template <int TYPE, int NV>
-__device__ __forceinline__ void list_vectors(const Chunk<TYPE, THREADS, NV> &k, const typename Kind<TYPE>::Val (&most)[NV], typename Kind<TYPE>::Val from, SharedVecs &vecs) {
+template <int TYPE, int T, int NV>
+__device__ __forceinline__ void list_vectors(const Chunk<TYPE, T, NV> &k, const typename Kind<TYPE>::Val (&most)[NV], typename Kind<TYPE>::Val from, SharedVecs &vecs) {
     uint32_t n = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) n += __popcll(__ballot(k.has(i) && !(most[i] < from)));
@@ -219,28 +223,29 @@ __device__ __forceinline__ void list_vectors(const Chunk<TYPE, THREADS, NV> &k, 
 }
 
 // Their elements to the list, a thread each.  Between two barriers of the caller.
-template <int TYPE>
+template <int TYPE, int T>
 __device__ __forceinline__ void list_elements(const SharedVecs &vecs, typename Kind<TYPE>::Val from, Shared &sh) {
     using K = Kind<TYPE>;
     constexpr int PV = PER_VEC<TYPE>;
     const uint32_t n = min(vecs.listed, (uint32_t)VECS) * PV;
-    for (uint32_t i0 = 0; i0 < n; i0 += THREADS) {
+    for (uint32_t i0 = 0; i0 < n; i0 += T) {
         const uint32_t i = i0 + threadIdx.x, j = min(i, n - 1);
         list_element(i < n, K::val(((const typename K::Raw *)vecs.raw)[j]), vecs.first[j / PV] + j % PV, from, sh);
     }
 }
 
 // A chunk of a row.
-template <int TYPE, int NV, bool TOP, bool ENT>
-__global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams p) {
+template <int TYPE, int T, int NV, bool TOP, bool ENT>
+__global__ __launch_bounds__(T) void logprobs_kernel(const LogprobsParams p) {
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>;
-    __shared__ __attribute__((aligned(16))) Shared sh;
+    __shared__ SharedStat<T> sums;
+    __shared__ __attribute__((aligned(16))) std::conditional_t<TOP, Shared, Nothing> sh;
     __shared__ __attribute__((aligned(16))) std::conditional_t<TOP, SharedVecs, Nothing> vecs;
     const uint32_t tid = threadIdx.x, row = blockIdx.x / p.chunks, chunk = blockIdx.x - row * p.chunks;
     const uint64_t r = p.row0 + row;
-    Chunk<TYPE, THREADS, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
+    Chunk<TYPE, T, NV> k(p.l, r, chunk, p.chunks, p.chunk_vecs);
     Given<TYPE> given;
     if (p.chunks == 1) given.load(p, r);
     const Val edge = K::val(k.edge);
@@ -272,7 +277,16 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
 #pragma unroll
         for (int e = 0; e < PV; ++e) add(v[e]);
     });
-    const Stat<Val> all = block_stat<THREADS, ENT>(a, c, sh, [&] { if (TOP) sh.key[tid] = key_of(a.m); });
+    const Stat<Val> all = block_stat<T, ENT>(a, c, sums, [&] {
+        if constexpr (TOP) {
+            uint32_t key = key_of(a.m);
+            if (T > KEYS) {
+                key = max(key, moved<0xB1>(key));
+                key = max(key, moved<0x4E>(key));
+            }
+            if (tid % (T / KEYS) == 0) sh.key[tid / (T / KEYS)] = key;
+        }
+    });
     if constexpr (TOP) {
         const uint32_t bound = key_bound<LOW_BITS<TYPE>>(sh, p.top);
         const Val from = of_key<Val>(max(bound, least_key<Val>()));
@@ -281,22 +295,22 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
         if (p.chunks == 1 || chunk == p.chunks - 1) list_element(k.edge_valid, edge, k.beside, from, sh);
         list_vectors(k, most, from, vecs);
         __syncthreads();
-        list_elements<TYPE>(vecs, from, sh);
+        list_elements<TYPE, T>(vecs, from, sh);
         if (vecs.listed > VECS && tid == 0) atomicMax(&sh.listed, LIST + 1u);   // some are missing: more than fit
         __syncthreads();
         const uint32_t listed = all.s == all.s ? sh.listed : 0;   // uniform; of a row with NaN nothing is asked for
         if (listed > p.list_cap && listed <= LIST) {   // neighbours that reach the bound together: of the listed, two a thread
-            const uint2 mine[2] = {tid < listed ? sh.list[tid] : make_uint2(0, 0), tid + THREADS < listed ? sh.list[tid + THREADS] : make_uint2(0, 0)};
+            const uint2 mine[2] = {tid < listed ? sh.list[tid] : make_uint2(0, 0), T < LIST && tid + T < listed ? sh.list[tid + T] : make_uint2(0, 0)};
             __syncthreads();
-            list_exactly([&](auto f) {
+            list_exactly<T>([&](auto f) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     if (mine[h].y) f(mine[h].x, ~mine[h].y);   // ~class is never 0
             }, p.top, sh);
         } else if (listed > LIST) {   // from memory again
             __syncthreads();
-            list_exactly([&](auto f) {
-                for (uint32_t j = k.first + tid * PV; j < k.first + k.n * PV; j += THREADS * PV) {
+            list_exactly<T>([&](auto f) {
+                for (uint32_t j = k.first + tid * PV; j < k.first + k.n * PV; j += T * PV) {
                     Val v[PV];
                     unpack<TYPE>(((const Loose *)(k.x + j))->v, v);
 #pragma unroll
@@ -309,14 +323,15 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(const LogprobsParams 
     }
     if (p.chunks == 1) {
         finish_values<TYPE>(p, r, all, given);
-        if constexpr (TOP) finish_top<TYPE>(p, r, all, sh);
+        if constexpr (TOP) finish_top<TYPE, T>(p, r, all, sh);
         return;
     }
     const size_t at = (size_t)row * p.chunks + chunk;
-    const uint32_t n = TOP && all.s == all.s ? sh.listed : 0;   // at most list_cap by now
+    uint32_t n = 0;
+    if constexpr (TOP) n = all.s == all.s ? sh.listed : 0;   // at most list_cap by now
     if (tid == 0) p.parts[at] = Part{__builtin_bit_cast(uint32_t, all.m), all.s, all.t, n};
     if constexpr (TOP)
-        for (uint32_t i = tid; i < n; i += THREADS) p.lists[at * p.list_cap + i] = sh.list[i];
+        for (uint32_t i = tid; i < n; i += T) p.lists[at * p.list_cap + i] = sh.list[i];
 }
 
 // Many rows with top alternatives: a workgroup goes through its row chunk by chunk, and no join is needed.  The bound of the
@@ -333,6 +348,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
     using K = Kind<TYPE>;
     using Val = typename K::Val;
     constexpr int PV = PER_VEC<TYPE>, OWN = VECS / THREADS;
+    __shared__ SharedStat<THREADS> sums;
     __shared__ __attribute__((aligned(16))) Shared sh;
     __shared__ __attribute__((aligned(16))) SharedVecs vecs;
     const uint32_t tid = threadIdx.x;
@@ -433,17 +449,17 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
     }
     Given<TYPE> given;
     given.load(p, r);
-    const Stat<Val> all = block_stat<THREADS, ENT>(a, c, sh, [] {});
+    const Stat<Val> all = block_stat<THREADS, ENT>(a, c, sums, [] {});
     Val most[OWN];
     raise_by_listed(most);
     list_element(edge_valid, edge, edge_class, from, sh);
-    list_elements<TYPE>(vecs, from, sh);
+    list_elements<TYPE, THREADS>(vecs, from, sh);
     __syncthreads();
     if ((lost || sh.listed > LIST) && all.s == all.s) {   // of a row with NaN nothing is asked for
         __syncthreads();
         const auto *x = (const typename K::Raw *)p.l.x + r * p.l.stride;
         const uint32_t whole = p.l.classes / PV * PV;
-        list_exactly([&](auto f) {
+        list_exactly<THREADS>([&](auto f) {
             for (uint32_t j = tid * PV; j < whole; j += THREADS * PV) {
                 Val v[PV];
                 unpack<TYPE>(((const Loose *)(x + j))->v, v);
@@ -458,7 +474,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
         }, p.top, sh);
     }
     finish_values<TYPE>(p, r, all, given);
-    finish_top<TYPE>(p, r, all, sh);
+    finish_top<TYPE, THREADS>(p, r, all, sh);
 }
 
 // The chunks of a row together: without top alternatives by a wave, with them by a workgroup.
@@ -527,10 +543,10 @@ __global__ __launch_bounds__(THREADS) void logprobs_top_join_kernel(const Logpro
     __syncthreads();
     if (sh.listed > LIST) {
         __syncthreads();
-        list_exactly(each, p.top, sh);
+        list_exactly<THREADS>(each, p.top, sh);
     }
     finish_values<TYPE>(p, p.row0 + row, all, given);
-    finish_top<TYPE>(p, p.row0 + row, all, sh);
+    finish_top<TYPE, THREADS>(p, p.row0 + row, all, sh);
 }
 
 // scale (sum_g u_g ([j = c_g] - p_j) - u_H p_j (log p_j + H))
@@ -819,10 +835,17 @@ static RowCut whole_rows(Way way, int type, uint32_t classes, uint64_t rows, uin
     return cut;
 }
 
-RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top) {
+// By chunks; up to `alone` rows of a size that many threads hold at once by a workgroup each, without a join.
+static RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, uint64_t alone) {
     RowCut cut{};
     const uint32_t vecs = vecs_of(type, classes);
     auto chunks_of = [&](uint32_t nv) { return (vecs + nv * THREADS - 1) / (nv * THREADS); };
+    if (vecs > 8 * THREADS && vecs <= 8 * ALONE && rows <= alone) {
+        cut = whole_rows(Way::alone, type, classes, rows, 1);
+        cut.nv = vecs <= 4 * ALONE ? 4 : 8;
+        cut.list_cap = LIST;
+        return cut;
+    }
     cut.way = Way::chunks;
     // Few rows: smaller chunks on more CUs, as long as the join still reads their lists at once
     cut.nv = vecs <= 2 * THREADS ? 2 : vecs > 8 * THREADS && rows * chunks_of(8) <= 512 && chunks_of(4) <= 16 && top ? 4 : 8;
@@ -859,23 +882,28 @@ RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top) {
     // 16 elements a lane at most.  100000 rows by a workgroup / by a wave, us: 257 f32 with entropy 98 / 30, with 5 alternatives
     // 267 / 85; 1024 f32 125 / 71, 273 / 148; 1024 bf16 111 / 49, 271 / 146
     if (classes <= 1024) return whole_rows(Way::wave, type, classes, rows, THREADS / 64);
-    return cut_rows(type, classes, rows, top);
+    // us by chunks and join / by a workgroup a row: 16 x 32000 bf16 with entropy and 20 alternatives 11.4 / 8.7, without 6.4 / 5.3; 512 rows
+    // 18.6 / 16.6, 11.0 / 8.8; 1000 rows 26.3 / 31.2, 16.7 / 16.2; 512 x 50001 with them 23.5 / 23.7, 256: 15.9 / 11.2.  In
+    // registers of 16 vectors a thread it lost: 1 x 131072 with them 11.8 / 16.7.
+    return cut_rows(type, classes, rows, top, top == 0 ? 1023 : vecs_of(type, classes) <= 4 * ALONE ? 512 : 256);
 }
 
-RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top) {
+RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top, bool rest) {
     if (sixteen_lanes(classes, top, 256)) return whole_rows(Way::sixteen, type, classes, rows, THREADS / 16);
     // 100000 rows by four waves / by one, loss / with gradient, us: 257 f32 140, 193 / 90, 100; 1000 bf16 172, 254 / 114, 152
     if (vecs_of(type, classes) <= WAVE_VECS) return whole_rows(Way::wave, type, classes, rows, 1);
-    return cut_rows(type, classes, rows, 0);
+    // us by chunks and join / by a workgroup a row, 64 entries, rest / none: 64 x 32000 bf16 8.8 / 7.8, 7.3 / 5.1; 512: 14.5 / 12.5, 11.7 / 7.9;
+    // 1000: 21.4 / 22.0, 17.5 / 14.7
+    return cut_rows(type, classes, rows, 0, rest ? 512 : 1023);
 }
 
-template <int TYPE, int NV>
+template <int TYPE, int T, int NV>
 static void launch_chunks(const LogprobsParams &p, hipStream_t st) {
-    const dim3 grid(p.run * p.chunks), block(THREADS);
-    if (p.top && p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, true, true>), grid, block, 0, st, p);
-    else if (p.top) hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, true, false>), grid, block, 0, st, p);
-    else if (p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, false, true>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((logprobs_kernel<TYPE, NV, false, false>), grid, block, 0, st, p);
+    const dim3 grid(p.run * p.chunks), block(T);
+    if (p.top && p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, true, true>), grid, block, 0, st, p);
+    else if (p.top) hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, true, false>), grid, block, 0, st, p);
+    else if (p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, false, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, false, false>), grid, block, 0, st, p);
 }
 
 template <int TYPE, int E>
@@ -917,9 +945,14 @@ static void launch_rows(const LogprobsParams &p, Way way, uint32_t nv, hipStream
         else hipLaunchKernelGGL((logprobs_row_top_kernel<TYPE, 8, false>), grid, block, 0, st, p);
         return;
     }
-    if (nv == 2) launch_chunks<TYPE, 2>(p, st);
-    else if (nv == 4) launch_chunks<TYPE, 4>(p, st);
-    else launch_chunks<TYPE, 8>(p, st);
+    if (way == Way::alone) {
+        if (nv == 4) launch_chunks<TYPE, ALONE, 4>(p, st);
+        else launch_chunks<TYPE, ALONE, 8>(p, st);
+        return;
+    }
+    if (nv == 2) launch_chunks<TYPE, THREADS, 2>(p, st);
+    else if (nv == 4) launch_chunks<TYPE, THREADS, 4>(p, st);
+    else launch_chunks<TYPE, THREADS, 8>(p, st);
     if (p.chunks == 1) return;
     if (!p.top) hipLaunchKernelGGL((logprobs_join_kernel<TYPE>), grid, dim3(64), 0, st, p);
     else if (p.chunks <= 16 && p.list_cap <= 128) hipLaunchKernelGGL((logprobs_top_join_kernel<TYPE, 2>), grid, block, 0, st, p);

@@ -205,6 +205,22 @@ def test_top_alternatives_of_many_long_rows(isr, torch, kind, classes, top):
     close(r.entropy[some], h, plain.U * plain.SUM * (3 + 2 * math.log(classes)), "entropy")
 
 
+@pytest.mark.parametrize("kind,rows,classes,top", [("bf16", 515, 20011, 5), ("bf16", 300, 50021, 64), ("f16", 520, 32003, 128), ("f32", 600, 9001, 100),
+                                                   ("i32", 270, 20011, 20), ("bf16", 1025, 17001, 0), ("f32", 1024, 8207, 0), ("bf16", 3, 70003, 0)])
+def test_rows_by_chunks(isr, torch, kind, rows, classes, top):
+    """More rows, or longer ones, than go by a workgroup each; the special rows among them."""
+    rng = np.random.default_rng(classes)
+    dev, wide = make(torch, kind, rows, classes, classes)
+    special, special_wide = put(torch, kind, np.stack(list(special_rows(kind, classes, rng).values())[:rows]))
+    dev[:len(special)] = special
+    wide[:len(special)] = special_wide
+    print(kind, rows, classes, top, flush=True)
+    given = rng.integers(0, classes, (rows, 2))
+    check_logprobs(isr, torch, kind, dev, wide, scale_of(kind), given, top)
+    for rest in (False, True):
+        check_distill(isr, torch, kind, dev, wide, scale_of(kind), make_teacher(torch, rng, rows, classes, 9, rest), 1.0, rest)
+
+
 def test_more_rows_than_a_launch_takes(isr, torch):
     """Behind 2^22 workgroups the next launch goes on: rows on both sides against the same rows by themselves."""
     for classes, rows in ((260, (1 << 22) + 5), (1, (1 << 26) + 5)):
