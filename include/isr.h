@@ -248,7 +248,11 @@ int isr_logprobs_grad(const isr_logits *logits, const int32_t *given_device, uin
  *   rest == 0: q = softmax of the entries' v (any common offset is free): the teacher's law on
  *              its top classes
  *   rest == 1: v are log-probabilities (isr_logprobs' top_logprob): q_i = exp v_i, and what they
- *              leave, q_rest = max(0, 1 - sum q_i), belongs to all other classes together */
+ *              leave, q_rest = max(0, 1 - sum q_i), belongs to all other classes together.  Where the
+ *              student's p_rest is 0 in fp32 (below 2^-150; no other class possible, or none left), a
+ *              q_rest that the rounding of the v explains is 0: up to h (E + scale 2^-14) + 2^-24 (top
+ *              + 16 + 4 E), E = -sum q_i log q_i, h half a step of their type (f32 2^-24, bf16 2^-8, f16
+ *              2^-11).  A larger one makes the loss +infinity there */
 typedef struct isr_teacher {
     const int32_t *class_device; /* [rows][top] */
     const void *logit_device;    /* [rows][top] */

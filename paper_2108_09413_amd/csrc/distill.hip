@@ -18,6 +18,16 @@ __device__ __forceinline__ float teacher_value(const void *p, int type, uint64_t
     return Kind<ISR_F16>::val(((const _Float16 *)p)[i]);
 }
 
+// Where the entries hold all of the teacher's probability, 1 - sum q is what rounding leaves of it, as often above 0 as below.  A student
+// whose other classes are impossible (or that has none) would be infinitely far off for that, one that masks them by a low number 1e-8 of
+// that number.  So q_rest is 0 where p_rest is 0 in fp32 too and 1 - sum q can be rounding alone: that of the values as they are stored,
+// and of their making in fp32, a sum of up to `top` exponentials, a logarithm and a difference.  e = -sum q_i log q_i.
+constexpr double NO_REST = -104.0;   // below log 2^-150
+__device__ __forceinline__ bool no_rest(const DistillParams &p, double left, double log_p, double e) {
+    const double half = p.value_type == ISR_F32 ? 0x1p-24 : p.value_type == ISR_BF16 ? 0x1p-8 : 0x1p-11;   // a step's, relative; below 2^-14 f16's stay
+    return log_p < NO_REST && left <= half * (e + p.value_scale * 0x1p-14) + 0x1p-24 * (p.top + 16 + 4 * e);
+}
+
 // ---- the entries of a row, by one wave, two a lane ------------------------------------------
 
 template <int TYPE>
@@ -144,13 +154,26 @@ __device__ __forceinline__ DistillStat conclude(const DistillParams &p, uint64_t
     }
     loss = wave_sum(loss);
     if (!p.rest) loss /= t.total;   // the q are rounded to 24 bits, and a sum of theirs above 1 would take a loss near the largest number to infinity
-    if (t.left > 0.0) {
+    double total = t.total, left = t.left;
+    if (left > 0.0) {
         const double lr = a.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(a.m, all.m) + ((double)rest_logs - logs);
-        loss += t.left * (logf((float)t.left) - lr);
+        double e_share = 0.0;
+        if (lr < NO_REST) {   // the same for all lanes
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (t.q[h] > 0.f) e_share -= (double)t.q[h] * t.logq(p, e.v[h]);
+            e_share = wave_sum(e_share);
+        }
+        if (no_rest(p, left, lr, e_share)) {
+            total -= left;
+            left = 0.0;
+        } else {
+            loss += left * (logf((float)left) - lr);
+        }
     }
     const bool bad = t.bad || all.s != all.s;
     if (writes) p.loss[r] = bad ? __builtin_nanf("") : (float)loss;
-    return DistillStat{bits_of(all.m), empty && !bad ? NEG_INF : logs, bits_of(a.m), rest_logs, t.value_m, t.value_logs, bad ? __builtin_nanf("") : (float)t.total, (float)t.left};
+    return DistillStat{bits_of(all.m), empty && !bad ? NEG_INF : logs, bits_of(a.m), rest_logs, t.value_m, t.value_logs, bad ? __builtin_nanf("") : (float)total, (float)left};
 }
 
 // ---- gradient ---------------------------------------------------------------------------------
@@ -465,7 +488,12 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
         if (!p.rest) loss /= total;   // as in conclude()
         if (left > 0.0) {
             const double lr = a.s == 0.f ? (double)NEG_INF : (double)p.l.scale * below64(a.m, all.m) + ((double)rest_logs - logs);
-            loss += left * (logf((float)left) - lr);
+            if (no_rest(p, left, lr, -entropy)) {
+                total -= left;
+                left = 0.0;
+            } else {
+                loss += left * (logf((float)left) - lr);
+            }
         }
         const bool nan = bad || all.s != all.s;
         st = DistillStat{bits_of(all.m), empty && !nan ? NEG_INF : logs, bits_of(a.m), rest_logs, value_m, value_logs,

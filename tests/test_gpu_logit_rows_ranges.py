@@ -1,0 +1,107 @@
+"""Operators on rows of class logits at the ends of their ranges: teachers that leave nothing to a rest class, sums over many chunks,
+log-probabilities next to the largest number, shares of the teacher next to zero, and workspaces of a larger call."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import logit_rows_plain as plain
+from test_gpu_logit_rows import TYPES, check_logprobs, close, dtype_of, grad_tol, isr, make, put, scale_of, torch  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}   # half a step, relative
+LOWEST = {"f32": -float(np.finfo(np.float32).max), "bf16": -2.0 ** 127 * (2 - 2.0 ** -7), "f16": -65504.0, "i32": -2.0 ** 31}
+
+
+def rest_rounding(v, top, kind, value_scale=1.0):
+    """How far 1 - sum exp v may lie from 0 by the rounding of v alone, as isr.h has it."""
+    e = -(np.exp(v) * v).sum()
+    return HALF[kind] * (e + value_scale * 2.0 ** -14) + 2.0 ** -24 * (top + 16 + 4 * e)
+
+
+def possible_rows(torch, kind, rows, classes, possible, mask, seed):
+    """Rows of which `possible` classes are ordinary and the others hold `mask`."""
+    dev, wide = make(torch, kind, rows, classes, seed)
+    rng = np.random.default_rng(seed)
+    for r in range(rows):
+        out = rng.permutation(classes)[possible:]
+        wide[r, out] = mask
+    return put(torch, kind, wide, pad=seed % 3)
+
+
+NOTHING_LEFT = [(kind, classes, classes, None) for kind in TYPES for classes in (1, 2, 10, 101, 128)] + [
+    (kind, classes, possible, mask) for kind, mask in (("f32", "-inf"), ("f32", "lowest"), ("f32", "-1e9"), ("bf16", "-inf"), ("bf16", "lowest"), ("f16", "-inf"), ("f16", "lowest"), ("i32", "lowest"))
+    for classes, possible in ((10, 4), (200, 20), (300, 20), (1000, 20), (5003, 100), (20011, 20), (70001, 20))]
+
+
+@pytest.mark.parametrize("stored_as", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind,classes,possible,mask", NOTHING_LEFT)
+def test_teachers_that_leave_nothing_to_the_rest(isr, torch, kind, classes, possible, mask, stored_as):
+    """A row's own stored log-probabilities of all its possible classes: they add up to 1 but for their rounding, so the rest class
+    has no share, and loss and gradient are those of the entries alone, whichever call makes them."""
+    rows, scale = 24, scale_of(kind)
+    low = LOWEST[kind] if mask == "lowest" else float(mask) if mask else 0.0
+    dev, wide = possible_rows(torch, kind, rows, classes, possible, low, classes)
+    top = min(classes, 128, possible + (3 if mask == "-inf" else 0))
+    print(kind, classes, possible, mask, stored_as, flush=True)
+    stored = isr.isr_logprobs(dev, top=top, scale=scale)
+    value = stored.top.to(dtype_of(torch, stored_as))
+    entry, v = stored.top_class.cpu().numpy(), value.double().cpu().numpy()
+    for r in range(rows):
+        there = entry[r] >= 0
+        assert there.sum() == possible and abs(1 - np.exp(v[r][there]).sum()) <= rest_rounding(v[r][there], top, stored_as)
+    check_rest(isr, torch, kind, dev, wide, scale, stored.top_class, value, True)
+    # a share that is more than rounding stays: a student without a class for it is infinitely far off
+    check_rest(isr, torch, kind, dev, wide, scale, stored.top_class, (value.float() - 0.1).to(value.dtype), False)
+
+
+def check_rest(isr, torch, kind, dev, wide, scale, cls, value, nothing):
+    """Loss and gradient, together and one after the other, of rows whose possible classes are all entries.  The others are all
+    alike, so each has its part of the rest class."""
+    entry, v = cls.cpu().numpy(), value.double().cpu().numpy()
+    rows, classes = wide.shape
+    loss, ltol, g, gtol = np.zeros(rows), np.zeros(rows), np.zeros((rows, classes)), np.zeros((rows, classes))
+    for r in range(rows):
+        there = entry[r] >= 0
+        c, w = entry[r][there], v[r][there]
+        logp, q = plain.row_logp(wide[r], scale)[0], np.exp(w)
+        left = 0.0 if nothing else 1 - q.sum()
+        other = np.ones(classes, dtype=bool)
+        other[c] = False
+        loss[r] = (q * (w - logp[c])).sum()
+        ltol[r] = (q * (2 * plain.logp_tol(logp[c]) + plain.U * (8 * np.abs(w) + 8))).sum()
+        if left > 0:
+            lr = logp[other].max() + math.log(other.sum()) if other.any() else -np.inf
+            loss[r] += left * (math.log(left) - lr)
+            ltol[r] += left * (2 * plain.logp_tol(lr) + plain.U * (8 * abs(math.log(left)) + 8))
+        ltol[r] += 4 * plain.U * abs(loss[r])
+        p, total = np.exp(logp[c]), q.sum() + left
+        g[r, c] = total * p - q
+        gtol[r, c] = plain.U * (total * p * (plain.SUM + 4 * np.abs(logp[c])) + q * (16 + 4 * np.abs(w)) + 4 * np.abs(g[r, c]))
+        if left > 0 and np.isfinite(wide[r, other]).all():
+            g[r, other] = -left / max(1, other.sum())
+            gtol[r, other] = plain.U * (plain.SUM + 8) * np.abs(g[r, other])
+    g, gtol = scale * g, grad_tol(kind, scale * g, scale * gtol)
+    a = isr.isr_distill(dev, cls, value, rest=True, scale=scale, stats=True)
+    b = isr.isr_distill(dev, cls, value, rest=True, scale=scale, grad=True)
+    close(a.loss, loss, ltol, "loss alone")
+    close(b.loss, loss, ltol, "loss with gradient")
+    close(b.grad, g, gtol, "gradient with loss")
+    close(isr.isr_distill_grad(dev, cls, value, a.stats, rest=True, scale=scale), g, gtol, "gradient alone")
+
+
+@pytest.mark.parametrize("classes,named", [(4, 4), (40, 4), (300, 4), (5000, 4)])
+def test_the_least_share_of_a_rest_class(isr, torch, classes, named):
+    """On both sides of the rounding that counts as nothing; a teacher's scale of 0.25 takes the values themselves four times as far."""
+    bound = rest_rounding(np.full(named, -math.log(named)), named, "f32", 0.25)
+    x = np.full((4, classes), -np.inf)
+    x[:, :named] = 0
+    dev, wide = put(torch, "f32", x)
+    e = torch.arange(named, dtype=torch.int32, device="cuda").repeat(4, 1)
+    left = np.array([-0.5, 0.25, 0.75, 1.5]) * bound
+    v = (4 * (-math.log(named) + np.log1p(-left)))[:, None].repeat(named, 1)
+    v32 = torch.from_numpy(v).float().cuda()
+    d = isr.isr_distill(dev, e, v32, rest=True, teacher_scale=0.25, grad=True)
+    assert torch.isfinite(d.loss[:3]).all() and (d.loss[:3].abs() <= 2 * bound).all()
+    assert d.loss[3] == math.inf and torch.isfinite(d.grad).all()
