@@ -334,6 +334,14 @@ __global__ __launch_bounds__(T) void logprobs_kernel(const LogprobsParams p) {
         for (uint32_t i = tid; i < n; i += T) p.lists[at * p.list_cap + i] = sh.list[i];
 }
 
+// 2^d, d <= 0.  A row that rises chunk by chunk multiplies its sum by one after the other, so next to 0 the difference from 1 is
+// right to a few half steps of itself: expm1's series, whose end is 2e-8 of it at -1/2.
+__device__ __forceinline__ double exp2_near_1(float d) {
+    const float x = d * LN2;
+    const float near = x + x * x * (0.5f + x * (1.f / 6 + x * (1.f / 24 + x * (1.f / 120 + x * (1.f / 720 + x * (1.f / 5040))))));
+    return d < -0.5f ? (double)__builtin_amdgcn_exp2f(d) : 1.0 + near;
+}
+
 // Many rows with top alternatives: a workgroup goes through its row chunk by chunk, and no join is needed.  The bound of the
 // first chunk serves until the listed vectors may want room; then, and at the end, it is raised to what `top` of the listed
 // reach, and those below are dropped.  A chunk with more than there is room for (a row that ascends) raises it to its own; rows with
@@ -354,7 +362,12 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
     const uint32_t tid = threadIdx.x;
     const uint64_t r = p.row0 + blockIdx.x;
     const float c = p.l.scale * LOG2E;
-    Stat<Val> a{lowest(Val()), 0.f, 0.f};
+    // A thread adds up its part of a chunk (64 terms) in fp32 and the chunks in 64 bits: one by one into a sum next to 1, the
+    // terms of a long flat tail are lost (262144 bf16 of which one is 17 above the others: log-probabilities off by 5e-5, 4194304: 4e-4).
+    Val m_all = lowest(Val());
+    __shared__ double sum[THREADS], weighted[ENT ? THREADS : 1];   // of each thread; in registers they cost a sixth of the waves
+    sum[tid] = 0.0;
+    if (ENT) weighted[tid] = 0.0;
     Val from = of_key<Val>(least_key<Val>());
     bool lost = false;     // candidates that found no room; this and the next are the same for all threads
     uint32_t listed = 0, added = 0;
@@ -418,7 +431,9 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
         edge = K::val(k.edge);
         edge_class = k.beside;
         edge_valid = k.edge_valid;
-        refer(a, larger(a.m, edge_valid ? larger(m, edge) : m), c);
+        Stat<Val> a{larger(m_all, edge_valid ? larger(m, edge) : m), 0.f, 0.f};
+        const float d = c * below(m_all, a.m);   // what there is so far is referred to the new maximum
+        m_all = a.m;
         auto add = [&](Val v) {
             const float d = c * below(v, a.m), e = __builtin_amdgcn_exp2f(d);
             a.s += e;
@@ -429,6 +444,9 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
 #pragma unroll
             for (int e = 0; e < PV; ++e) add(v[e]);
         });
+        const double f = exp2_near_1(d), s = sum[tid];
+        if (ENT) weighted[tid] = f * (weighted[tid] + fmaxf(d, NO_SHARE) * s) + a.t;
+        sum[tid] = f * s + a.s;
         k.keep_packed();
         if (chunk == 0) raise(key_of(m));
         else __syncthreads();   // all have read the count
@@ -449,7 +467,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
     }
     Given<TYPE> given;
     given.load(p, r);
-    const Stat<Val> all = block_stat<THREADS, ENT>(a, c, sums, [] {});
+    const Stat<Val> all = block_stat<THREADS, ENT>(Stat<Val>{m_all, (float)sum[tid], ENT ? (float)weighted[tid] : 0.f}, c, sums, [] {});
     Val most[OWN];
     raise_by_listed(most);
     list_element(edge_valid, edge, edge_class, from, sh);

@@ -105,3 +105,45 @@ def test_the_least_share_of_a_rest_class(isr, torch, classes, named):
     d = isr.isr_distill(dev, e, v32, rest=True, teacher_scale=0.25, grad=True)
     assert torch.isfinite(d.loss[:3]).all() and (d.loss[:3].abs() <= 2 * bound).all()
     assert d.loss[3] == math.inf and torch.isfinite(d.grad).all()
+
+
+@pytest.mark.parametrize("kind,classes", [("bf16", 262144), ("i32", 300007), ("f16", 1 << 22)])
+def test_one_class_above_a_long_flat_tail(isr, torch, kind, classes):
+    """Terms far smaller than the largest, many of them: a row of one class 15 to 17 above all others, in its first chunk, in the
+    middle, in its last.  More rows than go by chunks, so a workgroup goes through its row and adds up all of it."""
+    rows, unit = 1030, 1000 if kind == "i32" else 1
+    scale = 1.0 / unit
+    x = torch.zeros((rows, classes), dtype=dtype_of(torch, kind), device="cuda")
+    at = [0, 1, 255, 256 * 8, classes // 2, classes - 3000, classes - 1, classes - 8]
+    some = list(range(len(at))) + [rows - 1]
+    for r, j in enumerate(at + [77]):
+        x[some[r], j] = (15 + r % 3) * unit
+    print(kind, classes, flush=True)
+    given = torch.tensor((at + [77]), dtype=torch.int32, device="cuda")
+    all_given = torch.zeros((rows, 2), dtype=torch.int32, device="cuda")
+    all_given[some, 0] = given
+    all_given[some, 1] = (given + 5) % classes
+    r = isr.isr_logprobs(x, all_given, top=2, entropy=True, scale=scale, stats=True)
+    # by hand: one class of l, classes - 1 of 0
+    l = np.array([15 + k % 3 for k in range(len(some))], dtype=np.float64)
+    logz = np.log1p((classes - 1) * np.exp(-l))
+    want = np.stack([-logz, -l - logz], 1)
+    close(r.given[some], want, plain.logp_tol(want), "given")
+    close(r.top[some], want, plain.logp_tol(want), "top")
+    p = np.exp(want)
+    h = -p[:, 0] * want[:, 0] - (classes - 1) * p[:, 1] * want[:, 1]
+    close(r.entropy[some], h, plain.U * plain.SUM * (3 + 2 * math.log(classes)), "entropy")
+    close(r.stats[some, 1], logz, plain.logp_tol(logz), "statistics")
+
+
+def test_a_row_that_rises_chunk_by_chunk(isr, torch):
+    """Each chunk's largest a little above the last one's: the sum is referred to another maximum every time, and most of it is old."""
+    rows, classes = 1024, 1 << 20
+    x = torch.empty((rows, classes), device="cuda")
+    x[:] = torch.linspace(0, 0.5, classes, device="cuda")
+    r = isr.isr_logprobs(x, top=1, entropy=True)
+    lp, h, tc, tl = plain.logprobs(x[:1].double().cpu().numpy(), 1.0, None, 1)
+    assert (r.top_class == int(tc[0, 0])).all()
+    for k in (0, rows - 1):
+        close(r.top[k:k + 1], tl, plain.logp_tol(tl), "top")
+        close(r.entropy[k:k + 1], h, plain.U * plain.SUM * (3 + 2 * math.log(classes)), "entropy")
