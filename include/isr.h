@@ -222,6 +222,7 @@ typedef struct isr_logits {
  *   top_class_device      int32 [rows][top], top_logprob_device float [rows][top]: -1 and
  *                         -infinity from where the row has no further possible class
  *   stats_device          float [rows][2] or NULL: what isr_logprobs_grad reads
+ * A log-probability below fp32's lowest number is -infinity.
  * Empty row: log-probabilities -infinity, entropy 0.  ISR_ERR_ARG if nothing is asked for. */
 size_t isr_logprobs_workspace_bytes(const isr_logits *logits, uint32_t top);
 int isr_logprobs(const isr_logits *logits, const int32_t *given_device, uint32_t given, uint32_t top,

@@ -116,7 +116,12 @@ struct Logp {
     Val m;
     bool bad, empty;
     __device__ __forceinline__ Logp(const LogitRows &l, const Stat<Val> &a) : scale(l.scale), logs(a.s == 0.f ? 0.f : logf(a.s)), m(a.m), bad(a.s != a.s), empty(a.s == 0.f) {}
-    __device__ __forceinline__ float operator()(Val v) const { return bad ? __builtin_nanf("") : possible(v) ? scale * below(v, m) - logs : NEG_INF; }
+    __device__ __forceinline__ float operator()(Val v) const {
+        if (bad) return __builtin_nanf("");
+        if (!possible(v)) return NEG_INF;
+        const float d = below(v, m);
+        return d == NEG_INF ? (float)(scale * below64(v, m) - logs) : scale * d - logs;   // a difference beyond fp32, which the scale may bring back
+    }
 };
 
 // The given classes, one a thread of the first 64 or 128, read ahead of what their results wait for.

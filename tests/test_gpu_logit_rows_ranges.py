@@ -147,3 +147,21 @@ def test_a_row_that_rises_chunk_by_chunk(isr, torch):
     for k in (0, rows - 1):
         close(r.top[k:k + 1], tl, plain.logp_tol(tl), "top")
         close(r.entropy[k:k + 1], h, plain.U * plain.SUM * (3 + 2 * math.log(classes)), "entropy")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,classes", [(3, 10), (3, 200), (5, 300), (3, 3001), (3, 20011), (3, 140001), (1100, 20011)])
+def test_log_probabilities_further_down_than_logits_differ(isr, torch, kind, rows, classes):
+    """Logits of both ends of the type: their difference has no number, the log-probability at a scale below one half has."""
+    x = np.zeros((rows, classes))
+    x[:, classes // 2] = 3e38
+    x[:, 1] = -3e38
+    x[:, classes - 1] = -2e38
+    x[1] = np.where(np.arange(classes) % 2, 3e38, -3e38)
+    x[2, :] = -np.inf
+    x[2, [0, 3]] = 3e38, -3e38
+    dev, wide = put(torch, kind, x, pad=1)
+    given = np.tile(np.array([1, classes - 1, classes // 2, 3]), (rows, 1))
+    print(kind, rows, classes, flush=True)
+    for scale in (0.5, 0.25, 2.0 ** -20, 1e-30):
+        check_logprobs(isr, torch, kind, dev, wide, float(np.float32(scale)), given, min(classes, 6))
