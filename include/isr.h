@@ -185,8 +185,9 @@ size_t isr_noise_bank_static_capacity(void);
  * device memory, are enqueued on hip_stream (NULL = default; of the current device, which is the
  * one that holds the memory) and return at once: no allocation, no copy, no synchronisation, so
  * a call can be captured into a graph.  Workspaces (aligned to 16 bytes) hold nothing between calls; calls that may
- * overlap in time need a workspace each.  Sums and statistics are fp32 or wider.  Equal calls give
- * equal bits; the last bits of a row's sums may depend on the number of rows and on whether the
+ * overlap in time need a workspace each.  The size asked for some number of rows serves every smaller
+ * number too, of the same type, classes and other arguments.  Sums and statistics are fp32 or wider.  Equal
+ * calls give equal bits; the last bits of a row's sums may depend on the number of rows and on whether the
  * row starts at an even or an odd element.
  *
  * Results and workspace overlap neither each other nor what a call reads, but for gradients over

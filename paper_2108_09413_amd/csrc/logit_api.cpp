@@ -79,8 +79,7 @@ extern "C" {
 
 size_t isr_logprobs_workspace_bytes(const isr_logits *l, uint32_t top) {
     if (!valid_shape(l) || l->rows == 0 || top > ISR_MAX_TOP) return 0;
-    const RowCut cut = cut_logprobs(l->type, l->classes, l->rows, top);
-    return cut.parts_bytes + cut.lists_bytes;
+    return logprobs_workspace(l->type, l->classes, l->rows, top);
 }
 
 int isr_logprobs(const isr_logits *l, const int32_t *given_device, uint32_t given, uint32_t top, float *logprob_device,

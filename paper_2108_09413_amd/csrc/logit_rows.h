@@ -32,6 +32,7 @@ struct RowCut {
     size_t parts_bytes, lists_bytes;
 };
 RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top);
+size_t logprobs_workspace(int type, uint32_t classes, uint64_t rows, uint32_t top);   // bytes
 RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top, bool rest);
 RowCut cut_gradient(const LogitRows &l);
 

@@ -846,7 +846,9 @@ static bool sixteen_lanes(uint32_t classes, uint32_t serial, uint32_t most) {
 }
 
 static uint32_t vecs_of(int type, uint32_t classes) { return classes / (type == ISR_F32 || type == ISR_I32 ? 4 : 8); }
+static uint32_t chunks_of(uint32_t vecs, uint32_t nv) { return (vecs + nv * THREADS - 1) / (nv * THREADS); }
 constexpr uint32_t MOST_GROUPS = 1u << 22;   // of a launch
+constexpr uint32_t FEW_CHUNKS = 512;         // of a launch, that leave CUs idle
 
 // Rows whose workgroup (or its share) does them in one go, `groups` rows a workgroup.
 static RowCut whole_rows(Way way, int type, uint32_t classes, uint64_t rows, uint32_t groups) {
@@ -862,7 +864,6 @@ static RowCut whole_rows(Way way, int type, uint32_t classes, uint64_t rows, uin
 static RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, uint64_t alone) {
     RowCut cut{};
     const uint32_t vecs = vecs_of(type, classes);
-    auto chunks_of = [&](uint32_t nv) { return (vecs + nv * THREADS - 1) / (nv * THREADS); };
     if (vecs > 8 * THREADS && vecs <= 8 * ALONE && rows <= alone) {
         cut = whole_rows(Way::alone, type, classes, rows, 1);
         cut.nv = vecs <= 4 * ALONE ? 4 : 8;
@@ -871,8 +872,8 @@ static RowCut cut_rows(int type, uint32_t classes, uint64_t rows, uint32_t top, 
     }
     cut.way = Way::chunks;
     // Few rows: smaller chunks on more CUs, as long as the join still reads their lists at once
-    cut.nv = vecs <= 2 * THREADS ? 2 : vecs > 8 * THREADS && rows * chunks_of(8) <= 512 && chunks_of(4) <= 16 && top ? 4 : 8;
-    cut.chunks = chunks_of(cut.nv);
+    cut.nv = vecs <= 2 * THREADS ? 2 : vecs > 8 * THREADS && rows * chunks_of(vecs, 8) <= FEW_CHUNKS && chunks_of(vecs, 4) <= 16 && top ? 4 : 8;
+    cut.chunks = chunks_of(vecs, cut.nv);
     cut.chunk_vecs = (vecs + cut.chunks - 1) / cut.chunks;
     cut.chunks = (vecs + cut.chunk_vecs - 1) / cut.chunk_vecs;   // none of them empty
     if (top && cut.chunks > 1 && rows >= WHOLE_ROWS && (top <= WHOLE_TOP || cut.chunks <= WHOLE_CHUNKS)) cut.way = Way::row;
@@ -909,6 +910,17 @@ RowCut cut_logprobs(int type, uint32_t classes, uint64_t rows, uint32_t top) {
     // 18.6 / 16.6, 11.0 / 8.8; 1000 rows 26.3 / 31.2, 16.7 / 16.2; 512 x 50001 with them 23.5 / 23.7, 256: 15.9 / 11.2.  In
     // registers of 16 vectors a thread it lost: 1 x 131072 with them 11.8 / 16.7.
     return cut_rows(type, classes, rows, top, top == 0 ? 1023 : vecs_of(type, classes) <= 4 * ALONE ? 512 : 256);
+}
+
+// What the call with most need of 1 to `rows` rows takes.  It grows with the rows but where another way begins, behind FEW_CHUNKS and at
+// WHOLE_ROWS, where there may be none from there on.
+size_t logprobs_workspace(int type, uint32_t classes, uint64_t rows, uint32_t top) {
+    size_t most = 0;
+    for (const uint64_t ends : {rows, WHOLE_ROWS - 1, (uint64_t)FEW_CHUNKS / std::max(1u, chunks_of(vecs_of(type, classes), 8))}) {
+        const RowCut cut = cut_logprobs(type, classes, std::max<uint64_t>(1, std::min(rows, ends)), top);
+        most = std::max(most, cut.parts_bytes + cut.lists_bytes);
+    }
+    return most;
 }
 
 RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top, bool rest) {

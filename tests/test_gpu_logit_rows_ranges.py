@@ -165,3 +165,22 @@ def test_log_probabilities_further_down_than_logits_differ(isr, torch, kind, row
     print(kind, rows, classes, flush=True)
     for scale in (0.5, 0.25, 2.0 ** -20, 1e-30):
         check_logprobs(isr, torch, kind, dev, wide, float(np.float32(scale)), given, min(classes, 6))
+
+
+@pytest.mark.parametrize("kind,classes,top", [("bf16", 32000, 20), ("bf16", 131072, 20), ("f32", 20011, 3), ("bf16", 50021, 64)])
+def test_a_workspace_serves_all_smaller_batches(isr, torch, kind, classes, top):
+    """Of the size asked for 2048 rows once, for calls of fewer, with other memory behind it."""
+    L = isr.lib()
+    most = 2048
+    x = torch.randn((most, classes), device="cuda").to(dtype_of(torch, kind))
+    at = {"f32": isr.F32, "bf16": isr.BF16}[kind]
+    size = L.isr_logprobs_workspace_bytes(C.byref(isr.Logits(x.data_ptr(), at, classes, most, classes, 1.0)), top)
+    ws = torch.full((size + 256,), 77, dtype=torch.uint8, device="cuda")
+    want = isr.isr_logprobs(x, top=top)
+    for rows in (most, 1024, 1023, 700, 600, 513, 512, 257, 256, 129, 65, 64, 33, 32, 1):
+        tc, tl = torch.empty((rows, top), dtype=torch.int32, device="cuda"), torch.empty((rows, top), device="cuda")
+        l = isr.Logits(x.data_ptr(), at, classes, rows, classes, 1.0)
+        assert L.isr_logprobs(C.byref(l), None, 0, top, None, None, tc.data_ptr(), tl.data_ptr(), None, ws.data_ptr(), size, None) == isr.ISR_OK, rows
+        torch.cuda.synchronize()
+        assert torch.equal(tc, want.top_class[:rows]), rows
+    assert (ws[size:] == 77).all()
