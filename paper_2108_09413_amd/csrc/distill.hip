@@ -18,6 +18,16 @@ __device__ __forceinline__ float teacher_value(const void *p, int type, uint64_t
     return Kind<ISR_F16>::val(((const _Float16 *)p)[i]);
 }
 
+// log q and q of an entry of value v: the loss and the gradient from the statistics have the same bits.  With the rest class q is the
+// exponential in 64 bits, where 1 - sum q is next to 0; otherwise its exponent is rounded to fp32, off by |log q| half steps of q.
+__device__ __forceinline__ double log_share(const DistillParams &p, float v, float value_m, float value_logs) {
+    return (double)p.value_scale * ((double)v - value_m) - value_logs;
+}
+__device__ __forceinline__ float share_of(const DistillParams &p, float v, float value_m, float value_logs) {
+    const double lq = log_share(p, v, value_m, value_logs);
+    return p.rest ? (float)exp(lq) : expf((float)lq);
+}
+
 // Where the entries hold all of the teacher's probability, 1 - sum q is what rounding leaves of it, as often above 0 as below.  A student
 // whose other classes are impossible (or that has none) would be infinitely far off for that, one that masks them by a low number 1e-8 of
 // that number.  So q_rest is 0 where p_rest is 0 in fp32 too and 1 - sum q can be rounding alone: that of the values as they are stored,
@@ -82,7 +92,7 @@ struct Taught {
     float value_m, value_logs;
     bool is[2];           // first of its class
     bool none, bad;       // no teacher; no result
-    __device__ __forceinline__ double logq(const DistillParams &p, float v) const { return (double)p.value_scale * ((double)v - value_m) - value_logs; }
+    __device__ __forceinline__ double logq(const DistillParams &p, float v) const { return log_share(p, v, value_m, value_logs); }
 };
 template <int TYPE>
 __device__ __forceinline__ Taught taught(const DistillParams &p, const Entries<TYPE> &e, uint32_t *table) {
@@ -111,10 +121,10 @@ __device__ __forceinline__ Taught taught(const DistillParams &p, const Entries<T
     } else {
         float z = 0.f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) z += e.c[h] >= 0 ? expf((float)t.logq(p, e.v[h])) : 0.f;
+        for (int h = 0; h < 2; ++h) z += e.c[h] >= 0 ? share_of(p, e.v[h], t.value_m, 0.f) : 0.f;
         t.value_logs = logf(wave_sum(z));
 #pragma unroll
-        for (int h = 0; h < 2; ++h) t.q[h] = e.c[h] >= 0 ? expf((float)t.logq(p, e.v[h])) : 0.f;
+        for (int h = 0; h < 2; ++h) t.q[h] = e.c[h] >= 0 ? share_of(p, e.v[h], t.value_m, t.value_logs) : 0.f;
         t.total = wave_sum((double)t.q[0] + t.q[1]);
     }
     return t;
@@ -207,7 +217,7 @@ __global__ __launch_bounds__(T) void distill_grad_kernel(const DistillParams p) 
     Named named;
     named.load(p.entry + r * p.top, p.top);
     store_gradient(k, p.l.classes, (typename K::Grad *)p.grad + r * p.grad_stride, p.grad == p.l.x, row_slope<Val>(p, st, w), named, [&](int h) {
-        return expf(p.value_scale * (teacher_value(p.value, p.value_type, r * p.top + lane + 64 * h) - st.value_m) - st.value_logs);
+        return share_of(p, teacher_value(p.value, p.value_type, r * p.top + lane + 64 * h), st.value_m, st.value_logs);
     }, [&](Val v, float sum) { return entry_slope(p, st, w, v, sum); });
 }
 
@@ -413,7 +423,7 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
         if (none) value_m = 0.f;
         if (!p.rest) {
             float z = 0.f;
-            for (uint32_t i = lane; i < p.top; i += 16) z += ec[i] >= 0 ? expf(p.value_scale * (eq[i] - value_m)) : 0.f;
+            for (uint32_t i = lane; i < p.top; i += 16) z += ec[i] >= 0 ? share_of(p, eq[i], value_m, 0.f) : 0.f;
             value_logs = logf(sum16(z));
         }
     } else {
@@ -423,16 +433,16 @@ __global__ __launch_bounds__(THREADS) void distill_small_kernel(const DistillPar
     for (uint32_t i = lane; i < p.top; i += 16) {
         float share = 0.f;
         if (ec[i] >= 0) {
-            if (FORWARD && p.rest) {   // the sum that leads to q_rest in 64 bits
-                const double lq = (double)p.value_scale * (double)eq[i], full = exp(lq);
-                total += full;
-                share = (float)full;
-                if (share > 0.f) entropy += (double)share * lq;
+            const double lq = log_share(p, eq[i], value_m, value_logs);
+            if (p.rest) {   // the sum that leads to q_rest in 64 bits
+                const double full = exp(lq);
+                share = (float)full;   // as share_of()
+                if (FORWARD) total += full;
             } else {
-                const float lq = p.value_scale * (eq[i] - value_m) - value_logs;
-                share = expf(lq);
-                if (FORWARD && share > 0.f) { total += share; entropy += (double)share * lq; }
+                share = expf((float)lq);
+                if (FORWARD) total += share;
             }
+            if (FORWARD && share > 0.f) entropy += (double)share * lq;
         }
         eq[i] = share;
     }

@@ -184,3 +184,29 @@ def test_a_workspace_serves_all_smaller_batches(isr, torch, kind, classes, top):
         torch.cuda.synchronize()
         assert torch.equal(tc, want.top_class[:rows]), rows
     assert (ws[size:] == 77).all()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("kind", ["f32", "i32"])
+@pytest.mark.parametrize("classes", [10, 101, 200, 300, 3001, 20011, 70001])
+def test_small_shares_of_the_teacher(isr, torch, kind, classes, rest):
+    """A class that the student all but excludes has the teacher's share as its gradient: the same bits from the call that makes the
+    loss as from the statistics, and with the rest class (where a share is the exponential of what is stored) to the last places."""
+    rows, scale = 3, scale_of(kind)
+    x = np.zeros((rows, classes))
+    x[:, 2:5] = -200 / scale
+    dev, _ = put(torch, kind, x, pad=1)
+    e = torch.tensor([[1, 2, 3, 4]], dtype=torch.int32, device="cuda").repeat(rows, 1)
+    v = torch.tensor([[-0.02, -80.1, -33.7, -7.123], [-0.1, -50.3, -61.7, -20.9], [-0.05, -77.77, -3.3, -11.1]], device="cuda")
+    weight = torch.tensor([1.0, 2.0, 0.5], device="cuda")
+    a = isr.isr_distill(dev, e, v, weight=weight, rest=rest, scale=scale, teacher_scale=0.99, stats=True)
+    b = isr.isr_distill(dev, e, v, weight=weight, rest=rest, scale=scale, teacher_scale=0.99, grad=True)
+    c = isr.isr_distill_grad(dev, e, v, a.stats, weight=weight, rest=rest, scale=scale, teacher_scale=0.99)
+    assert torch.equal(b.grad[:, 2:5], c[:, 2:5])
+    lq = float(np.float32(0.99)) * v.double().cpu().numpy()
+    if not rest:
+        lq = lq - np.log(np.exp(lq).sum(1, keepdims=True))
+    want = -np.exp(lq[:, 1:]) * scale * weight.double().cpu().numpy()[:, None]
+    # rest: the share's rounding and two products'.  Otherwise its exponent in fp32 too, and the sum of shares
+    tol = np.abs(want) * plain.U * (4 if rest else 16 + 2 * np.abs(lq[:, 1:]))
+    close(b.grad[:, 2:5], want, tol, "gradient")
