@@ -16,8 +16,6 @@ CPU oracle timed on the host cores on a bounded sample of the same workload.
 from __future__ import annotations
 
 import argparse
-import glob
-import hashlib
 import json
 import os
 import re
@@ -44,13 +42,10 @@ OTHER_CONFIGS = ((0, 1024, 8), (1, 8192, 3), (2, 4096, 2), (3, 668, 3))
 
 
 def kernel_sources_sha256() -> str:
-    """Checksum of the kernel and host sources: an offline counter summary applies only to the code it was taken on."""
-    h = hashlib.sha256()
-    for path in sorted(glob.glob(os.path.join(ROOT, "paper_2108_09413_amd", "csrc", "*.*"))):
-        if path.endswith((".hip", ".h", ".cpp")):
-            h.update(os.path.basename(path).encode())
-            h.update(open(path, "rb").read())
-    return h.hexdigest()
+    """Checksum of the kernel and host sources that this benchmark runs: an offline counter summary applies only to the code it
+    was taken on."""
+    from paper_2108_09413_amd import profile_report
+    return profile_report.sources_sha256()
 
 
 def host_cpu_info() -> dict:
