@@ -932,13 +932,16 @@ RowCut cut_distill(int type, uint32_t classes, uint64_t rows, uint32_t top, bool
     return cut_rows(type, classes, rows, 0, rest ? 512 : 1023);
 }
 
+template <int TYPE, int T, int NV, bool TOP>
+static void launch_chunks_of(const LogprobsParams &p, hipStream_t st) {
+    const dim3 grid(p.run * p.chunks), block(T);
+    if (p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, TOP, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, TOP, false>), grid, block, 0, st, p);
+}
 template <int TYPE, int T, int NV>
 static void launch_chunks(const LogprobsParams &p, hipStream_t st) {
-    const dim3 grid(p.run * p.chunks), block(T);
-    if (p.top && p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, true, true>), grid, block, 0, st, p);
-    else if (p.top) hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, true, false>), grid, block, 0, st, p);
-    else if (p.entropy) hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, false, true>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((logprobs_kernel<TYPE, T, NV, false, false>), grid, block, 0, st, p);
+    if (p.top) launch_chunks_of<TYPE, T, NV, true>(p, st);
+    else launch_chunks_of<TYPE, T, NV, false>(p, st);
 }
 
 template <int TYPE, int E>
@@ -986,7 +989,7 @@ static void launch_rows(const LogprobsParams &p, Way way, uint32_t nv, hipStream
         return;
     }
     if (nv == 2) launch_chunks<TYPE, THREADS, 2>(p, st);
-    else if (nv == 4) launch_chunks<TYPE, THREADS, 4>(p, st);
+    else if (nv == 4) launch_chunks_of<TYPE, THREADS, 4, true>(p, st);   // cut_rows() takes it with alternatives only
     else launch_chunks<TYPE, THREADS, 8>(p, st);
     if (p.chunks == 1) return;
     if (!p.top) hipLaunchKernelGGL((logprobs_join_kernel<TYPE>), grid, dim3(64), 0, st, p);
