@@ -278,7 +278,8 @@ size_t isr_distill_workspace_bytes(const isr_logits *student, const isr_teacher 
 int isr_distill(const isr_logits *student, const isr_teacher *teacher, const float *row_weight_device,
                 float *loss_device, float *stats_device, void *grad_logits_device,
                 uint64_t grad_row_stride, void *workspace_device, size_t workspace_bytes, void *hip_stream);
-/* The gradient alone, from the statistics of an earlier call with the same student and teacher.
+/* The gradient alone, from the statistics of an earlier call with the same student and teacher; the
+ * teacher's shares in it have the same bits as in that call.
  * grad_logits_device as in isr_logprobs_grad. */
 int isr_distill_grad(const isr_logits *student, const isr_teacher *teacher, const float *row_weight_device,
                      const float *stats_device, void *grad_logits_device, uint64_t grad_row_stride,

@@ -453,6 +453,11 @@ def isr_float_debug_tensor(model: Model, x, sigma: float, seed: int, image_id: i
 
 
 # ---- operators on rows of class logits -----------------------------------------
+#
+# They take tensors on the device.  Results carry no graph of automatic differentiation, whether or not the logits require a gradient:
+# the gradients are results of their own (isr_logprobs_grad, isr_distill_grad, isr_distill(grad=...)), and a model behind the logits gets
+# its own by logits.backward(that gradient).  Networks of this library leave their logits on the host (isr_debug_forward,
+# isr_float_debug_forward), from where the caller takes them to the device.
 
 F32, BF16, F16, I32 = range(4)   # element types
 
@@ -542,7 +547,7 @@ def _grad_rows(x, out):
 
 def isr_logprobs(logits, given=None, top: int = 0, entropy: bool = False, scale: float = 1.0, stats: bool = False) -> LogProbs:
     """Log-probabilities of the given classes (int32 [rows, given], negative: does not count), entropy and top alternatives
-    of rows of logits, on the current stream of their device."""
+    of rows of logits, on the current stream of their device.  The results are detached: their gradient is isr_logprobs_grad."""
     import torch
     l = _logits(logits, scale)
     rows, n, f32 = logits.shape[0], 0, torch.float32
@@ -597,7 +602,8 @@ def _teacher(x, l, entry, value, scale, rest):
 def isr_distill(logits, teacher_class, teacher_logit, weight=None, rest: bool = False, scale: float = 1.0,
                 teacher_scale: float = 1.0, grad=False, stats: bool = False) -> Distilled:
     """Distillation loss of each row from a teacher's top logits (int32 and float [rows, top]; negative class: no entry).
-    weight (float32 [rows]): the gradient's factor.  grad: True, or the tensor it goes to (may be the logits themselves)."""
+    weight (float32 [rows]): the gradient's factor.  grad: True, or the tensor it goes to (may be the logits themselves).  The loss
+    is detached: a model that made the logits gets its gradients by logits.backward(r.grad)."""
     import torch
     l = _logits(logits, scale)
     t = _teacher(logits, l, teacher_class, teacher_logit, teacher_scale, rest)

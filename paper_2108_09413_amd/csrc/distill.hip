@@ -3,8 +3,8 @@
 // Loss alone: chunks of a row in registers, one workgroup each, and a join, as for the log-probabilities; with a rest class the
 // entries are left out of the chunks' sums; of few rows 1024 threads hold up to 8192 vectors, and no join follows.  Gradient alone: by elements from the row's statistics.
 // Both at once, rows that fit the registers of a workgroup (up to 16384 vectors of 16 bytes): the row is read once, held, and
-// its gradient stored from there, 4096 x 131072 bf16 with 64 entries and rest in 434 us (4.95 TB/s, of 5.8 that the
-// gradient alone reaches), 8192 x 32000 in 199 (5.3).  Longer rows take the two ways one after the other.
+// its gradient stored from there, 4096 x 131072 bf16 with 64 entries and rest in 458 us a call (4.7 TB/s, of 5.9 that the
+// gradient alone reaches), 8192 x 32000 in 206 (5.1).  Longer rows take the two ways one after the other, with three movements of the row.
 // Rows of up to 256 classes go by 16 lanes each unless they have many entries; rows of up to 256 vectors by a single wave.
 #include <algorithm>
 
@@ -131,7 +131,8 @@ __device__ __forceinline__ Taught taught(const DistillParams &p, const Entries<T
 }
 
 // Loss (stored) and statistics of a row, from the statistics of all classes or (rest) of those that are no entry.  The loss of a
-// student close to its teacher is a sum that cancels, so it is taken in 64 bits.
+// student close to its teacher is a sum that cancels, so its terms and their sum are in 64 bits; log Z and log q_rest in them are fp32's, off
+// by their rounding.
 template <int TYPE>
 __device__ __forceinline__ DistillStat conclude(const DistillParams &p, uint64_t r, const Stat<typename Kind<TYPE>::Val> &a, const Entries<TYPE> &e, const Taught &t) {
     using Val = typename Kind<TYPE>::Val;

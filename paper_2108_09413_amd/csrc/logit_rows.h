@@ -68,7 +68,7 @@ struct DistillStat {
     float m, logs;               // of all classes; m: as the logits' type holds it
     float rest_m, rest_logs;     // of those that are no entry (rest), else as m and logs
     float value_m, value_logs;   // q = exp(value_scale (value - value_m) - value_logs)
-    float total, left;           // sum of q and q_rest; q_rest
+    float total, left;           // sum of q and q_rest; q_rest, 0 where only rounding leaves one and there is no class for it
 };
 static_assert(sizeof(DistillStat) == 32, "eight words a row");
 

@@ -6,8 +6,8 @@
 // to 8192 by 1024 threads.  Of many rows with top alternatives a workgroup goes through all chunks of one.  Bound by memory: 4096 rows
 // of 131072 bf16 in 182 us, 5.9 TB/s, with 20 alternatives in 197.  Few rows are bound by latency: one row of 32000 bf16 with 20
 // alternatives and entropy takes 8.2 us, one of 131072 11.8 in two launches.
-// Gradient: element by element from the row's statistics, bound by memory too: 2048 x 65537 bf16 in 97 us, 5.5 TB/s; the few
-// named classes are stored behind the others.
+// Gradient: element by element from the row's statistics, bound by memory too: 2048 x 65537 bf16 with entropy in 91 us, 5.9 TB/s (97 a
+// call in a row of calls); the few named classes are stored behind the others.
 // Rows of up to 256 classes go by 16 lanes each, 100000 x 256 bf16 with entropy in 13 us (4.0 TB/s); of up to 1024 by a wave
 // each, 100000 x 1000 bf16 in 48 (4.2 TB/s).
 #include <algorithm>
@@ -351,8 +351,8 @@ __device__ __forceinline__ double exp2_near_1(float d) {
 // first chunk serves until the listed vectors may want room; then, and at the end, it is raised to what `top` of the listed
 // reach, and those below are dropped.  A chunk with more than there is room for (a row that ascends) raises it to its own; rows with
 // more candidates all the same (of many equal logits) are searched in memory.
-// us of a call with 20 / 64 / 128 alternatives, by chunks and join -> this way: 2048 x 32000 bf16 38 / 49 / 89 -> 33 / 39 / 47,
-// 2048 x 32771 f32 56 / 61 / 74 -> 47 / 54 / 63, 4096 x 131072 bf16 210 / 222 / 244 -> 197 / 235 / 247.  So: enough rows for four
+// us of a call with 20 / 64 / 128 alternatives, by chunks and join -> this way: 2048 x 32000 bf16 38 / 49 / 89 -> 33 / 38 / 46,
+// 2048 x 32771 f32 56 / 61 / 74 -> 48 / 53 / 59, 4096 x 131072 bf16 210 / 222 / 244 -> 197 / 235 / 247.  So: enough rows for four
 // workgroups a CU, and few alternatives or few chunks.
 constexpr uint64_t WHOLE_ROWS = 1024;
 constexpr uint32_t WHOLE_TOP = 32, WHOLE_CHUNKS = 5;
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_row_top_kernel(const Logprob
     const uint32_t tid = threadIdx.x;
     const uint64_t r = p.row0 + blockIdx.x;
     const float c = p.l.scale * LOG2E;
-    // A thread adds up its part of a chunk (64 terms) in fp32 and the chunks in 64 bits: one by one into a sum next to 1, the
+    // A thread adds up its part of a chunk (at most 64 terms) in fp32 and the chunks in 64 bits: one by one into a sum next to 1, the
     // terms of a long flat tail are lost (262144 bf16 of which one is 17 above the others: log-probabilities off by 5e-5, 4194304: 4e-4).
     Val m_all = lowest(Val());
     __shared__ double sum[THREADS], weighted[ENT ? THREADS : 1];   // of each thread; in registers they cost a sixth of the waves

@@ -210,3 +210,21 @@ def test_small_shares_of_the_teacher(isr, torch, kind, classes, rest):
     # rest: the share's rounding and two products'.  Otherwise its exponent in fp32 too, and the sum of shares
     tol = np.abs(want) * plain.U * (4 if rest else 16 + 2 * np.abs(lq[:, 1:]))
     close(b.grad[:, 2:5], want, tol, "gradient")
+
+
+def test_logits_that_a_model_made(isr, torch):
+    """Results are detached, and the gradient by the logits takes a model behind them to its own."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    w = torch.randn((50, 8), generator=gen, device="cuda", requires_grad=True)
+    x = torch.randn((16, 8), generator=gen, device="cuda")
+    e = torch.arange(4, dtype=torch.int32, device="cuda").repeat(16, 1)
+    v = torch.log_softmax(torch.randn((16, 4), generator=gen, device="cuda"), 1) - 0.1
+    logits = x @ w.t()
+    r = isr.isr_logprobs(logits, e, top=2, entropy=True, stats=True)
+    d = isr.isr_distill(logits, e, v, rest=True, grad=True)
+    assert not any(t.requires_grad for t in (*r, d.loss, d.grad))
+    logits.backward(d.grad)
+    want = d.grad.double().t() @ x.double()
+    # a product of 16 terms in fp32
+    assert bool(((w.grad.double() - want).abs() <= 17 * plain.U * (d.grad.double().abs().t() @ x.double().abs())).all())
